@@ -405,6 +405,100 @@ int nd_layer_edges_status(const void* workspace_dev, void* hip_stream);
 int nd_samples_pack(const int32_t* const* step_out_dev, int32_t num_steps, const int64_t* step_len,
                     int64_t num_samples, int32_t* samples_dev, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * From samples to training: rows of features, in device memory, one row of d numbers per vertex, sample or slot.
+ * `dtype` is an nd_dtype and the same for all rows of a call; a row's numbers lie next to each other, rows a fixed
+ * number of elements (`*_stride`, at least d) apart, at any address that is a multiple of the type's size.  Sums are
+ * held in 32-bit floats and rounded once, to nearest, ties to even.  All calls are asynchronous on hip_stream, allocate nothing, never
+ * wait and can be captured into a graph; equal inputs give equal outputs, bit for bit.  Pointers belong to the current
+ * device.  Outputs must not overlap inputs.
+ */
+typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
+#define ND_MAX_ROW 8192     /* numbers in a row */
+#define ND_MAX_LABELS 64    /* labels of a row of the softmax loss */
+#define ND_MAX_ROW_SLOTS 65536 /* slots of a row */
+
+/*
+ * Softmax loss over all vertices, the objective of walk embeddings (DeepWalk, node2vec: a centre predicts the vertices
+ * around it on its walk) and, with one label, of any model that answers with a vertex or a word.  Row n of x is scored
+ * against every row v of w; labels are vertices, NULL (negative) ones do not count, so step arrays of nd_sample serve as
+ * they are.  With s_nv = x_n . w_v and c_n the number of row n's labels that count:
+ *
+ *   lse_n  = log sum_v exp s_nv
+ *   loss_n = c_n lse_n - sum_j s_n,label[n][j]
+ *   dx_n   = row_weight_n (c_n sum_v p_nv w_v - sum_j w_label[n][j]),      p_nv = exp(s_nv - lse_n)
+ *   dw_v   = sum_n row_weight_n (c_n p_nv - #{j: label[n][j] = v}) x_n
+ *
+ * A row without labels that count is left out, whatever it holds: its loss, lse and dx are 0 and dw does not see it.
+ *
+ *   x_dev, w_dev     n rows and V rows of d numbers
+ *   labels_dev       n * k int32, below V
+ *   row_weight_dev   n float32: derivative of the total by each row's loss, e.g. 1 / number of pairs; NULL: 1
+ *   loss_dev, lse_dev   n float32 each
+ *   dx_dev, dw_dev   n rows and V rows of d numbers, every row written
+ *   workspace_dev    nd_softmax_loss_workspace_bytes bytes, 256-byte aligned, owned by the caller (grad: for
+ *                    nd_softmax_loss_grad); calls that overlap in time need one each
+ *
+ * Logits never exist as a whole: at most a piece of vertices at a time, in the workspace or in registers.  Their
+ * probabilities are rounded to the type of the rows before they are multiplied by rows.  A label of V
+ * or more counts as NULL and is recorded: nd_softmax_loss_status waits for the stream and returns ND_ERR_BAD_ROOT then.
+ * Limits: n < 2^30, V < 2^31, d <= ND_MAX_ROW, k <= ND_MAX_LABELS, n * k < 2^31.  Errors: ND_ERR_NULL_POINTER,
+ * ND_ERR_BAD_ARGUMENT, ND_ERR_TOO_LARGE, ND_ERR_WORKSPACE, ND_ERR_HIP.
+ */
+size_t nd_softmax_loss_workspace_bytes(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, int grad);
+int nd_softmax_loss(const void* x_dev, int64_t x_stride, const void* w_dev, int64_t w_stride, int dtype, int64_t n,
+                    int64_t V, int32_t d, const int32_t* labels_dev, int32_t k, float* loss_dev, float* lse_dev,
+                    void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+int nd_softmax_loss_grad(const void* x_dev, int64_t x_stride, const void* w_dev, int64_t w_stride, int dtype, int64_t n,
+                         int64_t V, int32_t d, const int32_t* labels_dev, int32_t k, const float* row_weight_dev,
+                         float* loss_dev, float* lse_dev, void* dx_dev, int64_t dx_stride, void* dw_dev,
+                         int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+int nd_softmax_loss_status(const void* workspace_dev, void* hip_stream);
+
+/*
+ * Rows in the order of nd_group_by_transit's groups, and back.  Slots belong to rows as in a step of k-hop: row r owns
+ * the slots r * m .. r * m + m - 1, and a slot's transit is the vertex (or relation type, or expert) that its copy of
+ * the row goes to.  Slots are numbers below n * m, n * m < 2^31.
+ *
+ * The pairs are sorted_slots_dev[0 .. n_pairs); where counts_dev is given (device, nd_group_by_transit's counts) only
+ * the first counts_dev[0] of them are live, and only the first counts_dev[1] of n_groups groups.  What lies behind the
+ * live ones in an output is left as it was.  weights_dev: n * m float32 by slot, or NULL for ones.  A slot or place out
+ * of range counts as none.
+ *
+ * nd_group_positions    position[q] = p where sorted_slots[p] = q, -1 for slots in no pair (n_slots int32)
+ * nd_rows_by_transit    out_p = weights[q] x_(q div m),  q = sorted_slots[p];  p in [0, pairs)
+ * nd_rows_to_samples    out_r = sum_j weights[r m + j] z_index[r m + j] over the places in [0, n_z), others are skipped
+ *                       whatever their weight; index = positions brings rows in group order back, index = sampled
+ *                       vertices sums their rows out of a table (a GraphSAGE aggregator; m = 1: a look-up)
+ * nd_rows_weight_grad   dweights[r m + j] = dy_r . z_index[r m + j], 0 where nd_rows_to_samples skips
+ * nd_rows_group_sum     out_u = sum over the pairs p of group u of weights[q] x_(q div m), q = sorted_slots[p], in the
+ *                       order of the pairs within pieces of equal size; the gradient of rows that several slots read.  group_row_dev NULL: out has
+ *                       n_groups rows; otherwise (device, nd_group_by_transit's group_transit: ascending) group u's sum is row
+ *                       group_row[u] of out, and the other of its out_rows rows are 0
+ *
+ * Gradients: of nd_rows_by_transit by x, nd_rows_to_samples of the incoming gradient over the positions; of
+ * nd_rows_to_samples by z, nd_rows_by_transit of the incoming gradient where index = positions, nd_rows_group_sum of it
+ * where places repeat, and by the weights, nd_rows_weight_grad.
+ * Errors: ND_ERR_NULL_POINTER, ND_ERR_BAD_ARGUMENT, ND_ERR_TOO_LARGE, ND_ERR_WORKSPACE, ND_ERR_HIP.
+ */
+int nd_group_positions(const int32_t* sorted_slots_dev, int64_t n_pairs, const int64_t* counts_dev, int64_t n_slots,
+                       int32_t* position_dev, void* hip_stream);
+int nd_rows_by_transit(const void* x_dev, int64_t x_stride, int dtype, int64_t n, int32_t d,
+                       const int32_t* sorted_slots_dev, int64_t n_pairs, const int64_t* counts_dev, int32_t m,
+                       const float* weights_dev, void* out_dev, int64_t out_stride, void* hip_stream);
+int nd_rows_to_samples(const void* z_dev, int64_t z_stride, int dtype, int64_t n_z, int32_t d, const int32_t* index_dev,
+                       int64_t n, int32_t m, const float* weights_dev, void* out_dev, int64_t out_stride,
+                       void* hip_stream);
+int nd_rows_weight_grad(const void* dy_dev, int64_t dy_stride, const void* z_dev, int64_t z_stride, int dtype,
+                        int64_t n_z, int32_t d, const int32_t* index_dev, int64_t n, int32_t m, float* dweights_dev,
+                        void* hip_stream);
+size_t nd_rows_group_sum_workspace_bytes(int64_t n_pairs, int32_t d);
+int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n, int32_t d,
+                      const int32_t* sorted_slots_dev, int64_t n_pairs, const int32_t* group_start_dev,
+                      int64_t n_groups, const int64_t* counts_dev, int32_t m, const float* weights_dev,
+                      const int32_t* group_row_dev, void* out_dev, int64_t out_stride, int64_t out_rows,
+                      void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
 /*
  * Phase timing, for measurement.  After nd_profile_enable(1) on a thread, the
  * nd_sample calls of that thread bracket every phase of every step with HIP

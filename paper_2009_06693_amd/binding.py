@@ -20,10 +20,16 @@ ND_MAX_FANOUT_STEPS = 8
 ND_MAX_WALK_STEPS = 4096
 ND_NULL_VERTEX = -1
 ND_MAX_EDGE_SLOTS = 2048
+ND_MAX_ROW = 8192
+ND_MAX_LABELS = 64
+ND_MAX_ROW_SLOTS = 65536
 
 ND_DEEPWALK, ND_PPR, ND_NODE2VEC, ND_KHOP, ND_LAYER, ND_MULTIRW = range(6)
 ND_MODE_TRANSIT_PARALLEL, ND_MODE_SAMPLE_PARALLEL = 0, 1
 ND_CLASS_AUTO, ND_CLASS_SUBWAVE, ND_CLASS_WORKGROUP, ND_CLASS_GRID = -1, 0, 1, 2
+
+ND_F32, ND_BF16, ND_F16 = range(3)
+_ROW_TYPES = {torch.float32: ND_F32, torch.bfloat16: ND_BF16, torch.float16: ND_F16}
 
 ND_OK = 0
 ND_ERR_NULL_POINTER, ND_ERR_BAD_ARGUMENT, ND_ERR_BAD_GRAPH, ND_ERR_BAD_WEIGHT = -1, -2, -3, -4
@@ -32,7 +38,10 @@ ND_ERR_NO_WEIGHTS, ND_ERR_WORKSPACE, ND_ERR_HIP, ND_ERR_BAD_ROOT, ND_ERR_TOO_LAR
 EXPORTS = ["nd_params_init", "nd_graph_create", "nd_graph_destroy", "nd_graph_info", "nd_sample_query",
            "nd_sample", "nd_sample_static", "nd_sample_status", "nd_sample_stats", "nd_group_workspace_bytes",
            "nd_group_by_transit", "nd_layer_edges_workspace_bytes", "nd_layer_edges_count",
-           "nd_layer_edges_fill", "nd_layer_edges_status", "nd_samples_pack", "nd_probe_store_runs", "nd_profile_enable", "nd_profile_read", "nd_last_error", "nd_version"]
+           "nd_layer_edges_fill", "nd_layer_edges_status", "nd_samples_pack", "nd_softmax_loss_workspace_bytes",
+           "nd_softmax_loss", "nd_softmax_loss_grad", "nd_softmax_loss_status", "nd_group_positions",
+           "nd_rows_by_transit", "nd_rows_to_samples", "nd_rows_weight_grad",
+           "nd_rows_group_sum_workspace_bytes", "nd_rows_group_sum", "nd_probe_store_runs", "nd_profile_enable", "nd_profile_read", "nd_last_error", "nd_version"]
 
 ND_PHASES = ["init", "sort", "group", "sample_sub", "sample_wg", "sample_sp", "layer", "unique", "walk_window"]
 
@@ -120,6 +129,29 @@ def lib() -> ctypes.CDLL:
         L.nd_layer_edges_status.argtypes = [vp, vp]
         L.nd_samples_pack.restype = ctypes.c_int
         L.nd_samples_pack.argtypes = [vp, i32, ctypes.POINTER(i64), i64, vp, vp]
+        L.nd_softmax_loss_workspace_bytes.restype = sz
+        L.nd_softmax_loss_workspace_bytes.argtypes = [i64, i64, i32, i32, ctypes.c_int, ctypes.c_int]
+        rows = [vp, i64]
+        L.nd_softmax_loss.restype = ctypes.c_int
+        L.nd_softmax_loss.argtypes = [*rows, *rows, ctypes.c_int, i64, i64, i32, vp, i32, vp, vp, vp, sz, vp]
+        L.nd_softmax_loss_grad.restype = ctypes.c_int
+        L.nd_softmax_loss_grad.argtypes = [*rows, *rows, ctypes.c_int, i64, i64, i32, vp, i32, vp, vp, vp, *rows, *rows,
+                                           vp, sz, vp]
+        L.nd_softmax_loss_status.restype = ctypes.c_int
+        L.nd_softmax_loss_status.argtypes = [vp, vp]
+        L.nd_group_positions.restype = ctypes.c_int
+        L.nd_group_positions.argtypes = [vp, i64, vp, i64, vp, vp]
+        L.nd_rows_by_transit.restype = ctypes.c_int
+        L.nd_rows_by_transit.argtypes = [*rows, ctypes.c_int, i64, i32, vp, i64, vp, i32, vp, *rows, vp]
+        L.nd_rows_to_samples.restype = ctypes.c_int
+        L.nd_rows_to_samples.argtypes = [*rows, ctypes.c_int, i64, i32, vp, i64, i32, vp, *rows, vp]
+        L.nd_rows_weight_grad.restype = ctypes.c_int
+        L.nd_rows_weight_grad.argtypes = [*rows, *rows, ctypes.c_int, i64, i32, vp, i64, i32, vp, vp]
+        L.nd_rows_group_sum_workspace_bytes.restype = sz
+        L.nd_rows_group_sum_workspace_bytes.argtypes = [i64, i32]
+        L.nd_rows_group_sum.restype = ctypes.c_int
+        L.nd_rows_group_sum.argtypes = [*rows, ctypes.c_int, i64, i32, vp, i64, vp, i64, vp, i32, vp, vp, *rows, i64, vp,
+                                        sz, vp]
         L.nd_probe_store_runs.restype = ctypes.c_int
         L.nd_probe_store_runs.argtypes = [vp, i64, i32, ctypes.c_int, vp]
         L.nd_profile_enable.restype = ctypes.c_int
@@ -387,6 +419,228 @@ def layer_edges(g: Graph, transits: torch.Tensor, sampled: torch.Tensor, stream=
     edge_slot = torch.empty(total, dtype=torch.int32, device=dev)
     nd_layer_edges_fill(g, transits, sampled, row_ptr, edge_slot, stream)
     return row_ptr, edge_slot
+
+
+# ---------------------------------------------------------------------------
+# Rows of features: 2-D CUDA tensors of float32, bfloat16 or float16 whose rows lie in one piece, at any stride.
+# ---------------------------------------------------------------------------
+
+def _on_device(t, what: str, dtype=None, entries: Optional[int] = None):
+    """The address of a contiguous tensor on the current device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{what} must be a contiguous CUDA tensor" + (f" of {dtype}" if dtype is not None else ""))
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} lies on device {t.get_device()} but device {torch.cuda.current_device()} is current")
+    if entries is not None and t.numel() < entries:
+        raise ValueError(f"{what} has {t.numel()} entries, {entries} are needed")
+    return t.data_ptr()
+
+
+def _rows(t, what: str, dtype=None, d: Optional[int] = None, n: Optional[int] = None):
+    """(address, stride) of rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype not in _ROW_TYPES:
+        raise TypeError(f"{what} must be a 2-D CUDA tensor of float32, bfloat16 or float16")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} lies on device {t.get_device()} but device {torch.cuda.current_device()} is current")
+    rows, cols = t.shape
+    if (dtype is not None and t.dtype != dtype) or (d is not None and cols != d) or (n is not None and rows != n):
+        raise ValueError(f"{what} is {rows} x {cols} of {t.dtype}, expected {rows if n is None else n} x "
+                         f"{cols if d is None else d} of {t.dtype if dtype is None else dtype}")
+    stride, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{what}: the numbers of a row must lie next to each other")
+    if rows > 1 and stride < cols:
+        raise ValueError(f"{what}: rows must not overlap")
+    return t.data_ptr(), (stride if rows > 1 else max(cols, 1))
+
+
+def _new(shape, dtype, device, stream):
+    """Memory for a call on that stream: in the stream's own order, so that what its last owner still does to it is over."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _optional(t, what: str, dtype, entries: int):
+    return None if t is None else _on_device(t, what, dtype, entries)
+
+
+def nd_softmax_loss_workspace_bytes(n: int, V: int, d: int, k: int, dtype: torch.dtype, grad: bool) -> int:
+    """Raises where the sizes are refused."""
+    size = lib().nd_softmax_loss_workspace_bytes(n, V, d, k, _ROW_TYPES.get(dtype, -1), int(grad))
+    if size == 0:
+        raise NdError(ND_ERR_BAD_ARGUMENT, lib().nd_last_error().decode())
+    return size
+
+
+def _loss_args(x, w, labels, loss, lse):
+    xp, xs = _rows(x, "x")
+    wp, wst = _rows(w, "w", x.dtype, x.shape[1])
+    n, d = x.shape
+    if not isinstance(labels, torch.Tensor) or labels.dim() not in (1, 2) or labels.shape[0] != n:
+        raise ValueError("labels must hold one row of labels per row of x")
+    k = labels.shape[1] if labels.dim() == 2 else 1
+    return (xp, xs, wp, wst, _ROW_TYPES[x.dtype], n, w.shape[0], d, _on_device(labels, "labels", torch.int32), k,
+            _on_device(loss, "loss", torch.float32, n), _on_device(lse, "lse", torch.float32, n))
+
+
+def nd_softmax_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                    workspace: torch.Tensor, stream=None):
+    """x [n, d], w [V, d], labels int32 [n] or [n, k]; loss and lse float32 [n] are written."""
+    xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep = _loss_args(x, w, labels, loss, lse)
+    _check(lib().nd_softmax_loss(xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep, _on_device(workspace, "workspace"),
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def nd_softmax_loss_grad(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, row_weight: Optional[torch.Tensor],
+                         loss: torch.Tensor, lse: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor],
+                         workspace: torch.Tensor, stream=None):
+    """As nd_softmax_loss; row_weight float32 [n] or None; dx [n, d] and dw [V, d] are written (None: not wanted)."""
+    xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep = _loss_args(x, w, labels, loss, lse)
+    dxp, dxs = (None, d) if dx is None else _rows(dx, "dx", x.dtype, d, n)
+    dwp, dws = (None, d) if dw is None else _rows(dw, "dw", x.dtype, d, V)
+    _check(lib().nd_softmax_loss_grad(xp, xs, wp, wst, dt, n, V, d, lp, k,
+                                      _optional(row_weight, "row_weight", torch.float32, n), op, ep, dxp, dxs, dwp, dws,
+                                      _on_device(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                      _stream_ptr(stream)))
+
+
+def nd_softmax_loss_status(workspace: torch.Tensor, stream=None):
+    _check(lib().nd_softmax_loss_status(workspace.data_ptr(), _stream_ptr(stream)))
+
+
+def _slots_of(n: int, m: int, t, what: str, dtype):
+    return None if t is None else _on_device(t, what, dtype, n * m)
+
+
+def _pairs(sorted_slots, counts):
+    return (_on_device(sorted_slots, "sorted_slots", torch.int32), sorted_slots.numel(),
+            _optional(counts, "counts", torch.int64, 2))
+
+
+def nd_group_positions(sorted_slots: torch.Tensor, n_slots: int, counts: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Where every slot's pair lies in sorted_slots (int32 [n_slots], -1: in no pair).  counts: what the grouping left on
+    the device, where sorted_slots has room for more pairs than are live."""
+    sp, pairs, cp = _pairs(sorted_slots, counts)
+    if out is None:
+        out = _new(n_slots, torch.int32, sorted_slots.device, stream)
+    _check(lib().nd_group_positions(sp, pairs, cp, n_slots, _on_device(out, "out", torch.int32, n_slots),
+                                    _stream_ptr(stream)))
+    return out
+
+
+def nd_rows_by_transit(x: torch.Tensor, sorted_slots: torch.Tensor, m: int, weights: Optional[torch.Tensor] = None,
+                       counts: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Rows in the order of the groups: out[p] = weights[q] * x[q // m], q = sorted_slots[p].  weights float32 [n * m]."""
+    xp, xs = _rows(x, "x")
+    sp, pairs, cp = _pairs(sorted_slots, counts)
+    n, d = x.shape
+    if out is None:
+        out = _new((pairs, d), x.dtype, x.device, stream)
+    op, ost = _rows(out, "out", x.dtype, d, pairs)
+    _check(lib().nd_rows_by_transit(xp, xs, _ROW_TYPES[x.dtype], n, d, sp, pairs, cp, m,
+                                    _slots_of(n, m, weights, "weights", torch.float32), op, ost, _stream_ptr(stream)))
+    return out
+
+
+def _samples(index: torch.Tensor, m: int):
+    if m < 1 or not isinstance(index, torch.Tensor) or index.numel() % m != 0:
+        raise ValueError(f"index must hold {m} slots per row")
+    return _on_device(index, "index", torch.int32), index.numel() // m
+
+
+def nd_rows_to_samples(z: torch.Tensor, index: torch.Tensor, m: int, weights: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[r] = sum over j of weights[r * m + j] * z[index[r * m + j]]; places outside [0, len(z)) are skipped."""
+    zp, zs = _rows(z, "z")
+    ip, n = _samples(index, m)
+    d = z.shape[1]
+    if out is None:
+        out = _new((n, d), z.dtype, z.device, stream)
+    op, ost = _rows(out, "out", z.dtype, d, n)
+    _check(lib().nd_rows_to_samples(zp, zs, _ROW_TYPES[z.dtype], z.shape[0], d, ip, n, m,
+                                    _slots_of(n, m, weights, "weights", torch.float32), op, ost, _stream_ptr(stream)))
+    return out
+
+
+def nd_rows_weight_grad(dy: torch.Tensor, z: torch.Tensor, index: torch.Tensor, m: int,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[r * m + j] = dy[r] . z[index[r * m + j]] (float32), 0 where nd_rows_to_samples skips."""
+    zp, zs = _rows(z, "z")
+    ip, n = _samples(index, m)
+    dyp, dys = _rows(dy, "dy", z.dtype, z.shape[1], n)
+    if out is None:
+        out = _new(n * m, torch.float32, z.device, stream)
+    _check(lib().nd_rows_weight_grad(dyp, dys, zp, zs, _ROW_TYPES[z.dtype], z.shape[0], z.shape[1], ip, n, m,
+                                     _on_device(out, "out", torch.float32, n * m), _stream_ptr(stream)))
+    return out
+
+
+def nd_rows_group_sum_workspace_bytes(n_pairs: int, d: int) -> int:
+    return lib().nd_rows_group_sum_workspace_bytes(n_pairs, d)
+
+
+def nd_rows_group_sum(x: torch.Tensor, sorted_slots: torch.Tensor, group_start: torch.Tensor, m: int,
+                      weights: Optional[torch.Tensor] = None, group_rows: Optional[torch.Tensor] = None,
+                      num_rows: Optional[int] = None, counts: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """Sums per group of weights[q] * x[q // m]; group_start int32 [groups + 1].  With group_rows (int32 [groups],
+    ascending: the grouping's transits) the sums are those rows of a table of num_rows, whose other rows are 0."""
+    xp, xs = _rows(x, "x")
+    sp, pairs, cp = _pairs(sorted_slots, counts)
+    gp = _on_device(group_start, "group_start", torch.int32, 1)
+    n, d = x.shape
+    groups = group_start.numel() - 1
+    if group_rows is None:
+        num_rows = groups if out is None else out.shape[0]
+    elif num_rows is None and out is None:
+        raise ValueError("group_rows need num_rows or out")
+    elif num_rows is None:
+        num_rows = out.shape[0]
+    if out is None:
+        out = _new((num_rows, d), x.dtype, x.device, stream)
+    op, ost = _rows(out, "out", x.dtype, d, num_rows)
+    rp = _optional(group_rows, "group_rows", torch.int32, groups)
+    if group_rows is not None and groups == 0:
+        rp = op  # an empty tensor has no address; it is not read
+    wsb = nd_rows_group_sum_workspace_bytes(pairs, d)
+    if workspace is None:
+        workspace = _new(wsb, torch.uint8, x.device, stream)
+    _check(lib().nd_rows_group_sum(xp, xs, _ROW_TYPES[x.dtype], n, d, sp, pairs, gp, groups, cp, m,
+                                   _slots_of(n, m, weights, "weights", torch.float32),
+                                   rp, op, ost, num_rows,
+                                   _on_device(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                   _stream_ptr(stream)))
+    return out
+
+
+class SoftmaxLoss:
+    """Workspace and outputs of the softmax loss for calls of one shape."""
+
+    def __init__(self, n: int, V: int, d: int, k: int, dtype: torch.dtype, grad: bool = False, device="cuda:0"):
+        self.workspace_bytes = nd_softmax_loss_workspace_bytes(n, V, d, k, dtype, grad)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+        self._loss = torch.empty(n, dtype=torch.float32, device=device)
+        self._lse = torch.empty(n, dtype=torch.float32, device=device)
+        self._dx = torch.empty((n, d), dtype=dtype, device=device) if grad else None
+        self._dw = torch.empty((V, d), dtype=dtype, device=device) if grad else None
+
+    def loss(self, x, w, labels, stream=None):
+        """(loss, lse) per row."""
+        nd_softmax_loss(x, w, labels, self._loss, self._lse, self.workspace, stream)
+        return self._loss, self._lse
+
+    def grad(self, x, w, labels, row_weight=None, stream=None):
+        """(loss, lse, dx, dw)."""
+        nd_softmax_loss_grad(x, w, labels, row_weight, self._loss, self._lse, self._dx, self._dw, self.workspace, stream)
+        return self._loss, self._lse, self._dx, self._dw
+
+    def status(self, stream=None):
+        nd_softmax_loss_status(self.workspace, stream)
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,645 @@
+// Rows of features along the grouping of slots by transit: into the order of the groups, back to the samples with
+// weights, summed per group, and the gradient of the weights.  Slot q belongs to row q / m, as the slots of a k-hop
+// step belong to their parents.
+//
+//     by transit    out[p] = w[q] x[q / m],                 q = sorted_slots[p]
+//     to samples    out[r] = sum_j w[r m + j] z[index[r m + j]]
+//     weight grad   dw[r m + j] = dy[r] . z[index[r m + j]]
+//     group sum     out[u] = sum over group u's pairs of w[q] x[q / m]
+//
+// Every one is bound by the rows it moves.  A lane holds 16 bytes of a row and the lanes of a workgroup are dealt out
+// over (row, piece) without gaps, so that rows of any length use all lanes; a row's last piece reaches back over the one
+// before it where the length is no multiple of a piece (both write the same numbers), and rows shorter than a piece go
+// number by number.  Sums are 32-bit, in an order that sizes alone decide; no atomics.
+#include <type_traits>
+
+#include "nd_philox.h"
+#include "nd_rowtypes.h"
+#include "nd_wave.h"
+
+namespace nd {
+namespace {
+
+constexpr int kThreads = 256;
+
+// A workgroup's lanes over rows and pieces: lane -> (row within the workgroup, piece of it).
+struct Deal {
+    FastDiv pieces;       // pieces of a row that one workgroup holds (at most kThreads)
+    uint32_t all_pieces;  // pieces of a row
+    uint32_t rows;        // rows of a workgroup
+    uint32_t lanes;       // rows * pieces
+};
+inline Deal make_deal(int32_t d, int vec) {
+    Deal t;
+    t.all_pieces = (uint32_t)((d + vec - 1) / vec);
+    const uint32_t here = t.all_pieces < kThreads ? t.all_pieces : kThreads;
+    t.pieces = make_fastdiv(here);
+    t.rows = kThreads / here;
+    t.lanes = t.rows * here;
+    return t;
+}
+// A launch holds fewer than 2^32 lanes, so workgroups go on to further rows from here on.
+constexpr int64_t kMaxGroups = 1 << 20;
+inline unsigned workgroups(int64_t n) { return (unsigned)(n < kMaxGroups ? n : kMaxGroups); }
+inline unsigned deal_threads(const Deal& t) { return (t.lanes + 63u) / 64u * 64u; }
+inline unsigned deal_columns(const Deal& t) { return (t.all_pieces + t.pieces.d - 1) / t.pieces.d; }
+
+// Where this lane's piece starts; false where the lane has none.
+template <int VEC>
+__device__ __forceinline__ bool deal_lane(const Deal& t, int32_t d, uint32_t* row, int32_t* at) {
+    *row = fastdiv(threadIdx.x, t.pieces);
+    const uint32_t piece = blockIdx.y * t.pieces.d + (threadIdx.x - *row * t.pieces.d);
+    const int32_t start = (int32_t)piece * VEC;
+    *at = start + VEC <= d ? start : d - VEC;
+    return threadIdx.x < t.lanes && piece < t.all_pieces;
+}
+
+// Live pairs: all of them, or as many as the grouping found.
+__device__ __forceinline__ int64_t live(int64_t all, const int64_t* counts, int which) {
+    if (!counts) return all;
+    const int64_t c = counts[which];
+    return c < all ? (c > 0 ? c : 0) : all;
+}
+
+__global__ __launch_bounds__(kThreads) void positions_clear_kernel(int32_t* __restrict__ position, int64_t n_slots) {
+    const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (q < n_slots) position[q] = -1;
+}
+__global__ __launch_bounds__(kThreads) void positions_kernel(const int32_t* __restrict__ slots, int64_t n_pairs,
+                                                             const int64_t* __restrict__ counts, int64_t n_slots,
+                                                             int32_t* __restrict__ position) {
+    const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (p >= live(n_pairs, counts, 0)) return;
+    const uint32_t q = (uint32_t)slots[p];
+    if (q < n_slots) position[q] = (int32_t)p;
+}
+
+template <typename T, int VEC, int ROUNDS>
+__global__ __launch_bounds__(kThreads) void by_transit_kernel(const T* __restrict__ x, int64_t x_stride, int32_t d, Deal t,
+                                                              const int32_t* __restrict__ slots, int64_t n_pairs,
+                                                              const int64_t* __restrict__ counts, FastDiv m,
+                                                              uint32_t n_slots, const float* __restrict__ weights,
+                                                              T* __restrict__ out, int64_t out_stride) {
+    uint32_t row;
+    int32_t at;
+    if (!deal_lane<VEC>(t, d, &row, &at)) return;
+    const int64_t pairs = live(n_pairs, counts, 0);
+    for (int64_t p0 = (int64_t)blockIdx.x * (ROUNDS * t.rows) + row; p0 < pairs; p0 += (int64_t)gridDim.x * (ROUNDS * t.rows)) {
+        uint32_t q[ROUNDS];
+        Piece<T, VEC> v[ROUNDS];
+        float w[ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int64_t p = p0 + (int64_t)i * t.rows;
+            q[i] = p < pairs ? (uint32_t)slots[p] : ~0u;
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            v[i] = Piece<T, VEC>{};
+            w[i] = 1.f;
+            if (q[i] < n_slots) {
+                v[i] = load_piece<T, VEC>(x + (int64_t)fastdiv(q[i], m) * x_stride + at);
+                if (weights) w[i] = weights[q[i]];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int64_t p = p0 + (int64_t)i * t.rows;
+            if (p >= pairs) break;
+            if (weights && q[i] < n_slots) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[i].v[e] = (T)((float)v[i].v[e] * w[i]);
+            }
+            store_piece<T, VEC>(out + p * out_stride + at, v[i]);
+        }
+    }
+}
+
+// A lane adds up its piece of the m rows, eight loads under way at a time.
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void to_samples_kernel(const T* __restrict__ z, int64_t z_stride, uint32_t n_z, int32_t d,
+                                                              Deal t, const int32_t* __restrict__ index, int64_t n, int32_t m,
+                                                              const float* __restrict__ weights, T* __restrict__ out,
+                                                              int64_t out_stride) {
+    constexpr int kAhead = 8;
+    uint32_t row;
+    int32_t at;
+    if (!deal_lane<VEC>(t, d, &row, &at)) return;
+    for (int64_t r = (int64_t)blockIdx.x * t.rows + row; r < n; r += (int64_t)gridDim.x * t.rows) {
+        const int32_t* idx = index + r * m;
+        const float* w = weights ? weights + r * m : nullptr;
+        float sum[VEC] = {};
+        for (int32_t j0 = 0; j0 < m; j0 += kAhead) {
+            uint32_t place[kAhead];
+            Piece<T, VEC> v[kAhead];
+            float f[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) place[i] = j0 + i < m ? (uint32_t)idx[j0 + i] : ~0u;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                v[i] = Piece<T, VEC>{};
+                f[i] = 0.f;
+                if (place[i] < n_z) {
+                    v[i] = load_piece<T, VEC>(z + (int64_t)place[i] * z_stride + at);
+                    f[i] = w ? w[j0 + i] : 1.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] = fmaf(f[i], (float)v[i].v[e], sum[e]);
+        }
+        Piece<T, VEC> o;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
+        store_piece<T, VEC>(out + r * out_stride + at, o);
+    }
+}
+
+// 2^log_lanes lanes of a wavefront share the dot products of one row with four of its slots' rows.
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void weight_grad_kernel(const T* __restrict__ dy, int64_t dy_stride,
+                                                               const T* __restrict__ z, int64_t z_stride, uint32_t n_z,
+                                                               int32_t d, const int32_t* __restrict__ index, int64_t n,
+                                                               int32_t m, int32_t quads, int log_lanes,
+                                                               float* __restrict__ dweights) {
+    const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
+    const int64_t per = kThreads >> log_lanes, items = n * quads;
+    for (int64_t i0 = (int64_t)blockIdx.x * per; i0 < items; i0 += (int64_t)gridDim.x * per) {
+        const int64_t item = i0 + (threadIdx.x >> log_lanes);
+        const bool mine = item < items;
+        const int64_t r = mine ? item / quads : 0;
+        const int32_t j0 = (int32_t)(item - r * quads) * 4;
+        uint32_t place[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) place[i] = mine && j0 + i < m ? (uint32_t)index[r * m + j0 + i] : ~0u;
+        float dot[4] = {};
+        for (int32_t c = lane * VEC; mine && c < d; c += lanes * VEC) {
+            const int32_t at = c + VEC <= d ? c : d - VEC;  // the last piece reaches back; what was counted is skipped
+            const int32_t skip = c - at;
+            const Piece<T, VEC> a = load_piece<T, VEC>(dy + r * dy_stride + at);
+            Piece<T, VEC> b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                b[i] = Piece<T, VEC>{};
+                if (place[i] < n_z) b[i] = load_piece<T, VEC>(z + (int64_t)place[i] * z_stride + at);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (place[i] >= n_z) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (e >= skip) dot[i] = fmaf((float)a.v[e], (float)b[i].v[e], dot[i]);
+            }
+        }
+        for (int s = lanes >> 1; s > 0; s >>= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot[i] += __shfl_xor(dot[i], s);
+        if (mine && lane == 0)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j0 + i < m) dweights[r * m + j0 + i] = dot[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------- sums per group
+// Pairs are cut into tiles of equal length, whatever the groups: a hub's pairs are spread over as many workgroups as
+// they fill tiles.  A group inside one tile is summed there; of one that crosses tiles every tile leaves what it holds
+// (32-bit floats: `first` if the group began before the tile, `last` otherwise), and a second launch adds those up.
+constexpr int kTilePairs = 64;
+
+struct GroupSum {
+    const int32_t* slots;
+    const int32_t* start;
+    const int64_t* counts;
+    const int32_t* group_row;
+    int64_t n_pairs, n_groups, out_rows, out_stride;
+    int32_t* tile_group;  // group of a tile's first pair
+    float* parts;         // [tile][first, last][d]
+};
+__device__ __forceinline__ int64_t start_of(const GroupSum& g, int64_t u, int64_t pairs) {
+    const int64_t s = g.start[u];
+    return s < 0 ? 0 : (s < pairs ? s : pairs);
+}
+// Live pairs that are in a group.
+__device__ __forceinline__ int64_t grouped_pairs(const GroupSum& g, int64_t groups) {
+    const int64_t pairs = live(g.n_pairs, g.counts, 0);
+    return groups > 0 ? start_of(g, groups, pairs) : 0;
+}
+// Row of the output that group u's sum goes to, or -1.
+__device__ __forceinline__ int64_t row_of_group(const GroupSum& g, int64_t u) {
+    if (!g.group_row) return u;
+    const int64_t r = g.group_row[u];
+    return r >= 0 && r < g.out_rows ? r : -1;
+}
+
+__global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
+    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    int64_t first = 0, last = -1;  // tiles whose first pair is this group's
+    if (u < groups) {
+        const int64_t a = start_of(g, u, pairs), b = start_of(g, u + 1, pairs);
+        if (b > a) {
+            first = (a + kTilePairs - 1) / kTilePairs;
+            last = (b - 1) / kTilePairs;
+        }
+    }
+    // few: every lane its own; many (a hub): the wavefront together
+    uint64_t many = __ballot(last - first >= 8);
+    if (last - first < 8)
+        for (int64_t t = first; t <= last; ++t) g.tile_group[t] = (int32_t)u;
+    while (many) {
+        const int from = __ffsll((unsigned long long)many) - 1;
+        many &= many - 1;
+        const int64_t a = __shfl(first, from), b = __shfl(last, from), v = __shfl(u, from);
+        for (int64_t t = a + lane_id(); t <= b; t += kWave) g.tile_group[t] = (int32_t)v;
+    }
+}
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict__ x, int64_t x_stride, int32_t d, Deal t,
+                                                             FastDiv m, uint32_t n_slots,
+                                                             const float* __restrict__ weights, GroupSum g,
+                                                             T* __restrict__ out) {
+    constexpr int kAhead = 8;
+    uint32_t row;
+    int32_t at;
+    if (!deal_lane<VEC>(t, d, &row, &at)) return;
+    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * kTilePairs < pairs; tile += (int64_t)gridDim.x * t.rows) {
+        const int64_t p0 = tile * kTilePairs;
+        const int64_t p1 = p0 + kTilePairs < pairs ? p0 + kTilePairs : pairs;
+        int64_t u = (uint32_t)g.tile_group[tile];
+        if (u >= groups) u = groups - 1;
+        bool before = start_of(g, u, pairs) < p0;
+        int64_t end = start_of(g, u + 1, pairs);
+        float sum[VEC] = {};
+        for (int64_t p = p0; p < p1; p += kAhead) {
+            uint32_t q[kAhead];
+            Piece<T, VEC> v[kAhead];
+            float f[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) q[i] = p + i < p1 ? (uint32_t)g.slots[p + i] : ~0u;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                v[i] = Piece<T, VEC>{};
+                f[i] = 0.f;
+                if (q[i] < n_slots) {
+                    v[i] = load_piece<T, VEC>(x + (int64_t)fastdiv(q[i], m) * x_stride + at);
+                    f[i] = weights ? weights[q[i]] : 1.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (p + i >= p1) break;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] = fmaf(f[i], (float)v[i].v[e], sum[e]);
+                if (p + i + 1 < end && p + i + 1 < p1) continue;
+                // the group ends here, or the tile does
+                if (!before && end <= p1) {
+                    const int64_t r = row_of_group(g, u);
+                    if (r >= 0) {
+                        Piece<T, VEC> o;
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
+                        store_piece<T, VEC>(out + r * g.out_stride + at, o);
+                    }
+                } else {
+                    Piece<float, VEC> o;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) o.v[e] = sum[e];
+                    store_piece<float, VEC>(g.parts + (tile * 2 + (before ? 0 : 1)) * d + at, o);
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+                before = false;
+                while (end <= p + i + 1 && u + 1 < groups) {  // groups without pairs are passed over
+                    ++u;
+                    end = start_of(g, u + 1, pairs);
+                }
+            }
+        }
+    }
+}
+
+// Adds up what tiles left of a group, a workgroup's rows of lanes taking every rows-th tile of a group.
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t, GroupSum g, T* __restrict__ out) {
+    __shared__ float shared[kThreads * VEC];
+    uint32_t row;
+    int32_t at;
+    const bool mine = deal_lane<VEC>(t, d, &row, &at);
+    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    // a workgroup looks through 64 groups at a time and joins those that cross tiles; groups without pairs are zero rows
+    for (int64_t u0 = (int64_t)blockIdx.x * kWave; u0 < groups; u0 += (int64_t)gridDim.x * kWave) {
+        int64_t a = 0, b = 1;
+        if (u0 + lane_id() < groups) {
+            a = start_of(g, u0 + lane_id(), pairs);
+            b = start_of(g, u0 + lane_id() + 1, pairs);
+        }
+        // the same in every wavefront
+        uint64_t todo = __ballot(b <= a ? !g.group_row : a / kTilePairs != (b - 1) / kTilePairs);
+        while (todo) {
+            const int from = __ffsll((unsigned long long)todo) - 1;
+            todo &= todo - 1;
+            const int64_t ua = __shfl(a, from), ub = __shfl(b, from);
+            const int64_t t0 = ua / kTilePairs, t1 = ub > ua ? (ub - 1) / kTilePairs : -1;
+            float sum[VEC] = {};
+            if (mine)
+                for (int64_t k = t0 + row; k <= t1; k += t.rows) {
+                    const Piece<float, VEC> v = load_piece<float, VEC>(g.parts + (k * 2 + (k == t0 ? 1 : 0)) * d + at);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += v.v[e];
+                }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) shared[threadIdx.x * VEC + e] = sum[e];
+            __syncthreads();
+            if (mine && row == 0) {
+                for (uint32_t k = 1; k < t.rows; ++k)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += shared[(threadIdx.x + k * t.pieces.d) * VEC + e];
+                const int64_t r = row_of_group(g, u0 + from);
+                if (r >= 0) {
+                    Piece<T, VEC> o;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
+                    store_piece<T, VEC>(out + r * g.out_stride + at, o);
+                }
+            }
+        }
+    }
+}
+
+// Rows that no group names are zero: a workgroup marks the named ones of 256 rows and clears the others.
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void group_clear_kernel(int32_t d, GroupSum g, T* __restrict__ out) {
+    __shared__ uint32_t named[kThreads];
+    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t r0 = (int64_t)blockIdx.x * kThreads;
+    const int64_t r1 = r0 + kThreads < g.out_rows ? r0 + kThreads : g.out_rows;
+    int64_t lo = 0, hi = groups;  // first group with a row of r0 or more
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if ((int64_t)g.group_row[mid] < r0)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    named[threadIdx.x] = 0;
+    __syncthreads();
+    // rows ascend, so that at most as many groups as rows follow
+    const int64_t u = lo + threadIdx.x;
+    if (u < groups) {
+        const int64_t r = g.group_row[u];
+        const bool holds = start_of(g, u + 1, pairs) > start_of(g, u, pairs);
+        if (r >= r0 && r < r1 && holds) named[r - r0] = 1;
+    }
+    __syncthreads();
+    const int32_t per_row = (d + VEC - 1) / VEC;
+    for (int64_t r = r0 + wave_id(); r < r1; r += kThreads / kWave) {
+        if (named[r - r0]) continue;
+        for (int32_t c = lane_id(); c < per_row; c += kWave) {
+            const int32_t at = c * VEC + VEC <= d ? c * VEC : d - VEC;
+            store_piece<T, VEC>(out + r * g.out_stride + at, Piece<T, VEC>{});
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ launches
+template <typename F>
+int by_type(int dtype, F&& f) {
+    switch (dtype) {
+        case ND_F32: return f((float*)nullptr);
+        case ND_BF16: return f((bf16_t*)nullptr);
+        default: return f((f16_t*)nullptr);
+    }
+}
+// 16 bytes at a time, or single numbers where a row has fewer.
+template <typename T, typename F>
+int by_width(int32_t d, F&& f) {
+    constexpr int kWide = 16 / (int)sizeof(T);
+    if (d >= kWide) return f(std::integral_constant<int, kWide>());
+    return f(std::integral_constant<int, 1>());
+}
+
+int check_slots(int64_t n, int32_t m, int64_t n_pairs) {
+    if (n < 0 || n_pairs < 0 || m < 1) {
+        set_error("n and n_pairs must not be negative and m at least 1");
+        return ND_ERR_BAD_ARGUMENT;
+    }
+    if (m > ND_MAX_ROW_SLOTS || n >= (1ll << 31) || n * (int64_t)m >= (1ll << 31) || n_pairs >= (1ll << 31)) {
+        set_error("at most %d slots per row, and fewer than 2^31 slots and pairs per call", ND_MAX_ROW_SLOTS);
+        return ND_ERR_TOO_LARGE;
+    }
+    return ND_OK;
+}
+
+struct GroupSumPlan {
+    int64_t tiles;
+    size_t o_parts, total;
+};
+GroupSumPlan plan_group_sum(int64_t n_pairs, int32_t d) {
+    GroupSumPlan p;
+    p.tiles = (n_pairs + kTilePairs - 1) / kTilePairs;
+    p.o_parts = ((size_t)p.tiles * 4 + 255) / 256 * 256;
+    p.total = p.o_parts + (size_t)p.tiles * 2 * (size_t)d * 4 + 256;
+    return p;
+}
+
+}  // namespace
+}  // namespace nd
+
+using namespace nd;
+
+extern "C" {
+
+int nd_group_positions(const int32_t* sorted_slots_dev, int64_t n_pairs, const int64_t* counts_dev, int64_t n_slots,
+                       int32_t* position_dev, void* hip_stream) {
+    if (n_pairs < 0 || n_slots < 0) {
+        set_error("n_pairs and n_slots must not be negative");
+        return ND_ERR_BAD_ARGUMENT;
+    }
+    if (n_pairs >= (1ll << 31) || n_slots >= (1ll << 31)) {
+        set_error("fewer than 2^31 slots and pairs per call");
+        return ND_ERR_TOO_LARGE;
+    }
+    if ((n_pairs > 0 && !sorted_slots_dev) || (n_slots > 0 && !position_dev)) {
+        set_error("a required pointer is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    if (n_slots == 0) return ND_OK;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    hipLaunchKernelGGL(positions_clear_kernel, dim3((unsigned)((n_slots + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                       stream, position_dev, n_slots);
+    if (n_pairs > 0)
+        hipLaunchKernelGGL(positions_kernel, dim3((unsigned)((n_pairs + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                           stream, sorted_slots_dev, n_pairs, counts_dev, n_slots, position_dev);
+    ND_HIP_CHECK(hipGetLastError());
+    return ND_OK;
+}
+
+int nd_rows_by_transit(const void* x_dev, int64_t x_stride, int dtype, int64_t n, int32_t d,
+                       const int32_t* sorted_slots_dev, int64_t n_pairs, const int64_t* counts_dev, int32_t m,
+                       const float* weights_dev, void* out_dev, int64_t out_stride, void* hip_stream) {
+    int rc = check_row_type(dtype, d);
+    if (rc == ND_OK) rc = check_slots(n, m, n_pairs);
+    if (rc == ND_OK) rc = check_rows("x_dev", x_dev, n, d, x_stride, dtype);
+    if (rc == ND_OK) rc = check_rows("out_dev", out_dev, n_pairs, d, out_stride, dtype);
+    if (rc != ND_OK) return rc;
+    if (n_pairs > 0 && !sorted_slots_dev) {
+        set_error("sorted_slots_dev is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    if (n_pairs == 0) return ND_OK;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    return by_type(dtype, [&](auto* type) -> int {
+        using T = std::remove_pointer_t<decltype(type)>;
+        return by_width<T>(d, [&](auto width) -> int {
+            constexpr int VEC = decltype(width)::value;
+            constexpr int kRounds = 4;
+            const Deal t = make_deal(d, VEC);
+            const int64_t per = (int64_t)t.rows * kRounds;
+            hipLaunchKernelGGL((by_transit_kernel<T, VEC, kRounds>), dim3(workgroups((n_pairs + per - 1) / per), deal_columns(t)),
+                               dim3(deal_threads(t)), 0, stream, (const T*)x_dev, x_stride, d, t, sorted_slots_dev, n_pairs,
+                               counts_dev, make_fastdiv((uint32_t)m), (uint32_t)(n * m), weights_dev, (T*)out_dev, out_stride);
+            ND_HIP_CHECK(hipGetLastError());
+            return ND_OK;
+        });
+    });
+}
+
+int nd_rows_to_samples(const void* z_dev, int64_t z_stride, int dtype, int64_t n_z, int32_t d, const int32_t* index_dev,
+                       int64_t n, int32_t m, const float* weights_dev, void* out_dev, int64_t out_stride,
+                       void* hip_stream) {
+    int rc = check_row_type(dtype, d);
+    if (rc == ND_OK) rc = check_slots(n, m, n_z);
+    if (rc == ND_OK) rc = check_rows("z_dev", z_dev, n_z, d, z_stride, dtype);
+    if (rc == ND_OK) rc = check_rows("out_dev", out_dev, n, d, out_stride, dtype);
+    if (rc != ND_OK) return rc;
+    if (n > 0 && !index_dev) {
+        set_error("index_dev is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    if (n == 0) return ND_OK;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    return by_type(dtype, [&](auto* type) -> int {
+        using T = std::remove_pointer_t<decltype(type)>;
+        return by_width<T>(d, [&](auto width) -> int {
+            constexpr int VEC = decltype(width)::value;
+            const Deal t = make_deal(d, VEC);
+            hipLaunchKernelGGL((to_samples_kernel<T, VEC>), dim3(workgroups((n + t.rows - 1) / t.rows), deal_columns(t)),
+                               dim3(deal_threads(t)), 0, stream, (const T*)z_dev, z_stride, (uint32_t)n_z, d, t, index_dev,
+                               n, m, weights_dev, (T*)out_dev, out_stride);
+            ND_HIP_CHECK(hipGetLastError());
+            return ND_OK;
+        });
+    });
+}
+
+int nd_rows_weight_grad(const void* dy_dev, int64_t dy_stride, const void* z_dev, int64_t z_stride, int dtype,
+                        int64_t n_z, int32_t d, const int32_t* index_dev, int64_t n, int32_t m, float* dweights_dev,
+                        void* hip_stream) {
+    int rc = check_row_type(dtype, d);
+    if (rc == ND_OK) rc = check_slots(n, m, n_z);
+    if (rc == ND_OK) rc = check_rows("dy_dev", dy_dev, n, d, dy_stride, dtype);
+    if (rc == ND_OK) rc = check_rows("z_dev", z_dev, n_z, d, z_stride, dtype);
+    if (rc != ND_OK) return rc;
+    if (n > 0 && (!index_dev || !dweights_dev)) {
+        set_error("a required pointer is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    if (n == 0) return ND_OK;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    return by_type(dtype, [&](auto* type) -> int {
+        using T = std::remove_pointer_t<decltype(type)>;
+        return by_width<T>(d, [&](auto width) -> int {
+            constexpr int VEC = decltype(width)::value;
+            int log_lanes = 0;
+            while (log_lanes < 6 && (VEC << log_lanes) < d) ++log_lanes;
+            const int32_t quads = (m + 3) / 4;
+            const int64_t per = kThreads >> log_lanes;
+            hipLaunchKernelGGL((weight_grad_kernel<T, VEC>), dim3(workgroups((n * quads + per - 1) / per)), dim3(kThreads),
+                               0, stream, (const T*)dy_dev, dy_stride, (const T*)z_dev, z_stride, (uint32_t)n_z, d, index_dev,
+                               n, m, quads, log_lanes, dweights_dev);
+            ND_HIP_CHECK(hipGetLastError());
+            return ND_OK;
+        });
+    });
+}
+
+size_t nd_rows_group_sum_workspace_bytes(int64_t n_pairs, int32_t d) {
+    if (n_pairs < 0 || n_pairs >= (1ll << 31) || d < 1 || d > ND_MAX_ROW) return 0;
+    return plan_group_sum(n_pairs, d).total;
+}
+
+int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n, int32_t d,
+                      const int32_t* sorted_slots_dev, int64_t n_pairs, const int32_t* group_start_dev,
+                      int64_t n_groups, const int64_t* counts_dev, int32_t m, const float* weights_dev,
+                      const int32_t* group_row_dev, void* out_dev, int64_t out_stride, int64_t out_rows,
+                      void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_row_type(dtype, d);
+    if (rc == ND_OK) rc = check_slots(n, m, n_pairs);
+    if (rc != ND_OK) return rc;
+    if (n_groups < 0 || out_rows < 0) {
+        set_error("n_groups and out_rows must not be negative");
+        return ND_ERR_BAD_ARGUMENT;
+    }
+    if (!group_row_dev && out_rows < n_groups) {
+        set_error("%lld rows for %lld groups", (long long)out_rows, (long long)n_groups);
+        return ND_ERR_BAD_ARGUMENT;
+    }
+    if (out_rows >= (1ll << 31) || n_groups >= (1ll << 31)) {
+        set_error("fewer than 2^31 rows and groups");
+        return ND_ERR_TOO_LARGE;
+    }
+    rc = check_rows("x_dev", x_dev, n, d, x_stride, dtype);
+    if (rc == ND_OK) rc = check_rows("out_dev", out_dev, out_rows, d, out_stride, dtype);
+    if (rc != ND_OK) return rc;
+    const GroupSumPlan plan = plan_group_sum(n_pairs, d);
+    if ((n_pairs > 0 && !sorted_slots_dev) || (n_groups > 0 && !group_start_dev) || (n_groups > 0 && !workspace_dev)) {
+        set_error("a required pointer is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    if (n_groups > 0 && (workspace_bytes < plan.total || ((uintptr_t)workspace_dev % 256) != 0)) {
+        set_error("workspace needs %zu bytes aligned to 256", plan.total);
+        return ND_ERR_WORKSPACE;
+    }
+    if (out_rows == 0) return ND_OK;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    GroupSum g{};
+    g.slots = sorted_slots_dev;
+    g.start = group_start_dev;
+    g.counts = counts_dev;
+    g.group_row = group_row_dev;
+    g.n_pairs = n_pairs;
+    g.n_groups = n_groups;
+    g.out_rows = out_rows;
+    g.out_stride = out_stride;
+    g.tile_group = (int32_t*)workspace_dev;
+    g.parts = (float*)((char*)workspace_dev + plan.o_parts);
+    return by_type(dtype, [&](auto* type) -> int {
+        using T = std::remove_pointer_t<decltype(type)>;
+        return by_width<T>(d, [&](auto width) -> int {
+            constexpr int VEC = decltype(width)::value;
+            const Deal t = make_deal(d, VEC);
+            if (group_row_dev)
+                hipLaunchKernelGGL((group_clear_kernel<T, VEC>), dim3((unsigned)((out_rows + kThreads - 1) / kThreads)),
+                                   dim3(kThreads), 0, stream, d, g, (T*)out_dev);
+            if (n_groups > 0 && n_pairs > 0) {
+                hipLaunchKernelGGL(group_tiles_kernel, dim3((unsigned)((n_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                                   stream, g);
+                hipLaunchKernelGGL((group_sum_kernel<T, VEC>), dim3(workgroups((plan.tiles + t.rows - 1) / t.rows), deal_columns(t)),
+                                   dim3(deal_threads(t)), 0, stream, (const T*)x_dev, x_stride, d, t, make_fastdiv((uint32_t)m),
+                                   (uint32_t)(n * m), weights_dev, g, (T*)out_dev);
+            }
+            if (n_groups > 0)
+                hipLaunchKernelGGL((group_join_kernel<T, VEC>), dim3(workgroups((n_groups + kWave - 1) / kWave), deal_columns(t)),
+                                   dim3(deal_threads(t)), 0, stream, d, t, g, (T*)out_dev);
+            ND_HIP_CHECK(hipGetLastError());
+            return ND_OK;
+        });
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,760 @@
+// Softmax loss over all vertices and its gradient, in pieces of the vertices.
+//
+//     s_nv = x_n . w_v        lse_n = log sum_v exp s_nv        loss_n = c_n lse_n - sum_j s_n,label[n][j]
+//     dx_n = g_n (c_n sum_v p_nv w_v - sum_j w_label[n][j])     dw_v = sum_n g_n (c_n p_nv - #{j: label = v}) x_n
+//
+// Rows with labels are gathered once into a dense, zero-padded array, so that every product below works on full tiles of
+// rows that count, whatever rows without labels hold.  The logits are a matrix product whose tiles leave only a running
+// maximum and sum per row; for the gradient the tiles are made again, turned into g (c p - count), rounded to the rows'
+// type and multiplied by w (for dx) and by x (for dw), a piece of vertices at a time.
+#include <cfloat>
+#include <type_traits>
+
+#include "nd_rowtypes.h"
+#include "nd_wave.h"
+
+namespace nd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 128;         // rows and columns of a product's tile
+constexpr int kChunk = 16;         // bytes that a lane moves at once
+constexpr int kTileBytes = kTile * 128;  // one operand's tile: 128 bytes of the summed dimension
+constexpr size_t kPieceBytes = 512u << 20;  // probabilities that lie in the workspace at a time
+
+typedef float Acc __attribute__((ext_vector_type(16)));
+typedef short Short4 __attribute__((ext_vector_type(4)));
+
+struct LossHeader {
+    uint32_t status;   // bit 0: a label was V or more
+    uint32_t n_live;   // rows with labels
+    float scale;       // what probabilities are multiplied by before they are rounded, a power of two
+    uint32_t pad[61];
+};
+static_assert(sizeof(LossHeader) == 256, "one 256-byte block");
+
+// What the kernels share.  Arrays by place are those of the gathered rows.
+struct LossArgs {
+    int64_t n, V, n_pad;
+    int32_t d, dp, k;
+    const int32_t* labels;
+    const float* row_weight;
+    float *loss, *lse;        // by row
+    LossHeader* header;
+    uint32_t* block_live;     // per kTile rows: rows with labels,
+    float* block_weight;      // the largest weight among them,
+    uint32_t* block_bad;      // whether a label is V or more
+    int32_t* row_of;          // by place: row
+    float* count;             // by place: labels that count
+    float* weight;            // by place: row weight
+    float* place_lse;         // by place
+    float *part_max, *part_sum;  // [groups of vertices][n_pad]
+    int32_t groups;
+};
+
+__device__ __forceinline__ int32_t labels_of_row(const LossArgs& a, int64_t row, bool* bad) {
+    int32_t c = 0;
+    for (int32_t j = 0; j < a.k; ++j) {
+        const int32_t v = a.labels[row * a.k + j];
+        if (v >= 0) {
+            if ((int64_t)v < a.V)
+                ++c;
+            else
+                *bad = true;
+        }
+    }
+    return c;
+}
+
+__global__ __launch_bounds__(kTile) void count_kernel(LossArgs a) {
+    __shared__ uint32_t s_live[2], s_bad[2];
+    __shared__ float s_weight[2];
+    const int64_t row = (int64_t)blockIdx.x * kTile + threadIdx.x;
+    bool bad = false;
+    const bool live = row < a.n && labels_of_row(a, row, &bad) > 0;
+    float w = live ? (a.row_weight ? fabsf(a.row_weight[row]) : 1.f) : 0.f;
+    for (int s = 32; s > 0; s >>= 1) w = fmaxf(w, __shfl_xor(w, s));
+    const uint64_t lives = __ballot(live), bads = __ballot(bad);
+    if (lane_id() == 0) {
+        s_weight[wave_id()] = w;
+        s_live[wave_id()] = (uint32_t)__popcll(lives);
+        s_bad[wave_id()] = bads != 0;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        a.block_live[blockIdx.x] = s_live[0] + s_live[1];
+        a.block_bad[blockIdx.x] = s_bad[0] | s_bad[1];
+        a.block_weight[blockIdx.x] = fmaxf(s_weight[0], s_weight[1]);
+    }
+}
+
+// Gathers the rows with labels, zeroes what the others get, and pads to a whole tile.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* __restrict__ x, int64_t x_stride,
+                                                          T* __restrict__ rows, T* __restrict__ dx, int64_t dx_stride,
+                                                          int32_t blocks) {
+    __shared__ uint32_t s_before[4], s_all[4], s_bad[4], s_wave[2];
+    __shared__ float s_weight[4];
+    __shared__ int32_t s_row[kTile];
+    uint32_t before = 0, all = 0, bad_any = 0;
+    float top = 0.f;
+    for (int32_t b = threadIdx.x; b < blocks; b += kThreads) {
+        const uint32_t c = a.block_live[b];
+        all += c;
+        if (b < (int32_t)blockIdx.x) before += c;
+        bad_any |= a.block_bad[b];
+        top = fmaxf(top, a.block_weight[b]);
+    }
+    for (int s = 32; s > 0; s >>= 1) {
+        before += __shfl_xor(before, s);
+        all += __shfl_xor(all, s);
+        bad_any |= __shfl_xor(bad_any, s);
+        top = fmaxf(top, __shfl_xor(top, s));
+    }
+    if (lane_id() == 0) {
+        s_before[wave_id()] = before;
+        s_all[wave_id()] = all;
+        s_bad[wave_id()] = bad_any;
+        s_weight[wave_id()] = top;
+    }
+    const int64_t row0 = (int64_t)blockIdx.x * kTile;
+    int32_t c = 0;
+    if (threadIdx.x < kTile) {
+        bool bad = false;
+        if (row0 + threadIdx.x < a.n) c = labels_of_row(a, row0 + threadIdx.x, &bad);
+    }
+    const uint64_t lives = __ballot(c > 0);
+    if (threadIdx.x < kTile && lane_id() == 0) s_wave[wave_id()] = (uint32_t)__popcll(lives);
+    __syncthreads();
+    before = s_before[0] + s_before[1] + s_before[2] + s_before[3];
+    all = s_all[0] + s_all[1] + s_all[2] + s_all[3];
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        top = fmaxf(fmaxf(s_weight[0], s_weight[1]), fmaxf(s_weight[2], s_weight[3]));
+        a.header->status = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
+        a.header->n_live = all;
+        // fp16 holds 2^-24 to 65,504: the largest product of a weight and a count of labels becomes at most 2^15
+        float scale = 1.f;
+        if (std::is_same<T, f16_t>::value && top > 0.f && top < FLT_MAX)
+            scale = exp2f(fminf(fmaxf(floorf(log2f(32768.f / (float)a.k) - log2f(top)), -60.f), 60.f));
+        a.header->scale = scale;
+    }
+    const uint32_t here = s_wave[0] + s_wave[1];
+    if (threadIdx.x < kTile) {
+        const int64_t row = row0 + threadIdx.x;
+        const uint32_t at = (wave_id() == 1 ? s_wave[0] : 0u) + (uint32_t)__popcll(lives & lanes_below(lane_id()));
+        if (c > 0) {
+            s_row[at] = (int32_t)row;
+            a.row_of[before + at] = (int32_t)row;
+            a.count[before + at] = (float)c;
+            a.weight[before + at] = a.row_weight ? a.row_weight[row] : 1.f;
+        } else if (row < a.n) {
+            a.loss[row] = 0.f;
+            a.lse[row] = 0.f;
+        }
+    }
+    __syncthreads();
+    for (uint32_t r = wave_id(); r < here; r += 4) {
+        const T* from = x + (int64_t)s_row[r] * x_stride;
+        T* to = rows + (int64_t)(before + r) * a.dp;
+        for (int32_t e = lane_id(); e < a.dp; e += kWave) to[e] = e < a.d ? from[e] : (T)0.f;
+    }
+    if (dx)  // rows without labels
+        for (int32_t r = wave_id(); r < kTile && row0 + r < a.n; r += 4) {
+            bool dead = true;
+            for (int32_t j = 0; j < a.k; ++j) {
+                const int32_t v = a.labels[(row0 + r) * a.k + j];
+                if (v >= 0 && (int64_t)v < a.V) dead = false;
+            }
+            if (dead)
+                for (int32_t e = lane_id(); e < a.d; e += kWave) dx[(row0 + r) * dx_stride + e] = (T)0.f;
+        }
+    if ((int32_t)blockIdx.x == blocks - 1) {
+        const uint32_t padded = (all + kTile - 1) / kTile * kTile;
+        for (uint32_t p = all + threadIdx.x; p < padded; p += kThreads) {
+            a.row_of[p] = -1;
+            a.count[p] = 0.f;
+            a.weight[p] = 0.f;
+            a.place_lse[p] = 0.f;
+        }
+        for (int64_t e = (int64_t)all * a.dp + threadIdx.x; e < (int64_t)padded * a.dp; e += kThreads) rows[e] = (T)0.f;
+    }
+}
+
+// Rows of d numbers at any stride to rows of dp, zeros behind.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void pad_kernel(const T* __restrict__ w, int64_t stride, int64_t rows, int32_t d,
+                                                       int32_t dp, T* __restrict__ out) {
+    for (int64_t r = (int64_t)blockIdx.x * 4 + wave_id(); r < rows; r += (int64_t)gridDim.x * 4)
+        for (int32_t e = lane_id(); e < dp; e += kWave) out[r * dp + e] = e < d ? w[r * stride + e] : (T)0.f;
+}
+
+// ------------------------------------------------------------------------------------------------ product of tiles
+// C[m][n] = sum_k A(m, k) B(n, k) for a tile of 128 x 128, four wavefronts of 64 x 64 each in 32 x 32 matrix
+// instructions.  An operand lies in memory with the summed dimension along its rows (ACROSS = false) or down its columns
+// (ACROSS = true), and in LDS as it does in memory, 16-byte pieces of a row exchanged so that the reads of a
+// wavefront fall on different banks.
+template <typename T>
+struct Operand {
+    const T* base;
+    int64_t stride;
+    int64_t rows;   // of the array: reads behind it are of its last row
+    int32_t cols;   // ACROSS: numbers in a row (a multiple of a piece): pieces behind are the last one again
+};
+
+template <typename T>
+struct Kind {
+    static constexpr int kVec = kChunk / (int)sizeof(T);       // numbers in a piece
+    static constexpr int kStep = 128 / (int)sizeof(T);         // of the summed dimension in a tile
+    static constexpr bool kWide = sizeof(T) == 4;
+};
+
+// Byte position of piece c of row r in LDS.
+template <typename T, bool ACROSS>
+__device__ __forceinline__ int lds_place(int r, int c) {
+    if (!ACROSS) return (r * 8 + (c ^ ((r >> 1) & 7))) * kChunk;                               // 128 rows of 8 pieces
+    if (Kind<T>::kWide) return (r * 32 + (c ^ (((r >> 2) & 1) << 3))) * kChunk;                // 32 rows of 32 pieces
+    return (r * 16 + (c ^ (((r & 3) << 2) | ((r >> 2) & 3)))) * kChunk;                        // 64 rows of 16 pieces
+}
+
+struct Chunks {
+    uint4 v[4];
+};
+template <typename T, bool ACROSS>
+__device__ __forceinline__ void fetch(const Operand<T>& o, int64_t m0, int64_t k0, Chunks& c) {
+    constexpr int kPieces = ACROSS ? kTile / Kind<T>::kVec : 8;  // of a row of the tile
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = i * kThreads + (int)threadIdx.x, r = e / kPieces, p = e % kPieces;
+        int64_t row = (ACROSS ? k0 : m0) + r;
+        row = row < o.rows ? row : o.rows - 1;
+        int64_t col = (ACROSS ? m0 : k0) + p * Kind<T>::kVec;
+        if (ACROSS && col > o.cols - Kind<T>::kVec) col = o.cols - Kind<T>::kVec;
+        c.v[i] = *reinterpret_cast<const uint4*>(o.base + row * o.stride + col);
+    }
+}
+template <typename T, bool ACROSS>
+__device__ __forceinline__ void keep(char* lds, const Chunks& c) {
+    constexpr int kPieces = ACROSS ? kTile / Kind<T>::kVec : 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = i * kThreads + (int)threadIdx.x;
+        *reinterpret_cast<uint4*>(lds + lds_place<T, ACROSS>(e / kPieces, e % kPieces)) = c.v[i];
+    }
+}
+
+// A lane's share of a 32-row block for one group of the summed dimension: 16-bit types 16 of it, lane l holds row l % 32
+// and the eight from 8 (l / 32) on; fp32 8 of it, the four from 4 (l / 32) on, one for each of four instructions.
+template <typename T>
+struct Fragment {
+    T v[Kind<T>::kVec];
+};
+template <typename T, bool ACROSS>
+__device__ __forceinline__ Fragment<T> fragment(const char* lds, int block_row, int group) {
+    const int lane = lane_id(), half = lane >> 5;
+    Fragment<T> f;
+    if (!ACROSS) {
+        const int r = block_row + (lane & 31);
+        f = *reinterpret_cast<const Fragment<T>*>(lds + lds_place<T, false>(r, group * 2 + half));
+    } else if (Kind<T>::kWide) {
+        const int col = block_row + (lane & 31);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            f.v[e] = *reinterpret_cast<const T*>(lds + lds_place<T, true>(group * 8 + half * 4 + e, col / 4) + col % 4 * 4);
+    } else {
+        // 16 lanes hand in 4 rows x 16 columns and get a column of four rows each
+        const int sub = lane & 15, col = block_row + ((lane >> 4) & 1) * 16 + (sub & 3) * 4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = group * 16 + half * 8 + e * 4 + (sub >> 2);
+            const char* at = lds + lds_place<T, true>(r, col / 8) + (col & 4) * 2;
+            const Short4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) Short4*)at);
+            __builtin_memcpy(&f.v[e * 4], &t, 8);
+        }
+    }
+    return f;
+}
+__device__ __forceinline__ Acc multiply(const Fragment<float>& a, const Fragment<float>& b, Acc c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ Acc multiply(const Fragment<bf16_t>& a, const Fragment<bf16_t>& b, Acc c) {
+    typedef bf16_t V8 __attribute__((ext_vector_type(8)));
+    V8 x, y;
+    __builtin_memcpy(&x, &a, 16);
+    __builtin_memcpy(&y, &b, 16);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+}
+__device__ __forceinline__ Acc multiply(const Fragment<f16_t>& a, const Fragment<f16_t>& b, Acc c) {
+    typedef f16_t V8 __attribute__((ext_vector_type(8)));
+    V8 x, y;
+    __builtin_memcpy(&x, &a, 16);
+    __builtin_memcpy(&y, &b, 16);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
+}
+
+// The tile at (m0, n0) summed over [k0, k1), k1 - k0 a multiple of Kind::kStep; lds: 4 * kTileBytes.  Ends with a barrier.
+// Result: lane l of wavefront w holds column n = 64 (w % 2) + 32 j + l % 32 and rows m = 64 (w / 2) + 32 i + 8 (r / 4) +
+// 4 (l / 32) + r % 4 in acc[i][j][r].
+template <typename T, bool A_ACROSS, bool B_ACROSS>
+__device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0, int64_t k0,
+                                        int64_t k1, char* lds, Acc (&acc)[2][2]) {
+    constexpr int kGroups = Kind<T>::kWide ? 4 : 4;  // 32 / 8, 64 / 16
+    const int wm = wave_id() / 2 * 64, wn = wave_id() % 2 * 64;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = Acc{};
+    if (k0 >= k1) return;
+    Chunks ca, cb;
+    fetch<T, A_ACROSS>(a, m0, k0, ca);
+    fetch<T, B_ACROSS>(b, n0, k0, cb);
+    int buffer = 0;
+    for (int64_t k = k0; k < k1; k += Kind<T>::kStep) {
+        char* la = lds + buffer * 2 * kTileBytes;
+        char* lb = la + kTileBytes;
+        keep<T, A_ACROSS>(la, ca);
+        keep<T, B_ACROSS>(lb, cb);
+        __syncthreads();
+        if (k + Kind<T>::kStep < k1) {
+            fetch<T, A_ACROSS>(a, m0, k + Kind<T>::kStep, ca);
+            fetch<T, B_ACROSS>(b, n0, k + Kind<T>::kStep, cb);
+        }
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            Fragment<T> fa[2], fb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fa[i] = fragment<T, A_ACROSS>(la, wm + i * 32, g);
+                fb[i] = fragment<T, B_ACROSS>(lb, wn + i * 32, g);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fa[i], fb[j], acc[i][j]);
+        }
+        buffer ^= 1;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 64 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
+__device__ __forceinline__ int acc_col(int j) { return wave_id() % 2 * 64 + j * 32 + (lane_id() & 31); }
+
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// ------------------------------------------------------------------------------------------------------- forward
+// A workgroup takes 128 rows and every groups-th tile of vertices; a lane keeps maximum and sum of its two columns.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x) {
+    __shared__ __align__(16) char lds[4 * kTileBytes];
+    const int64_t n0 = (int64_t)blockIdx.x * kTile;
+    if (n0 >= (int64_t)a.header->n_live) return;
+    float top[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {};
+    for (int64_t v0 = (int64_t)blockIdx.y * kTile; v0 < a.V; v0 += (int64_t)a.groups * kTile) {
+        Acc acc[2][2];
+        product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float t = top[j];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (v0 + acc_row(i, r) >= a.V) acc[i][j][r] = -INFINITY;
+                    t = fmaxf(t, acc[i][j][r]);
+                }
+            float s = sum[j] * exp_of(top[j] - t);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += exp_of(acc[i][j][r] - t);
+            top[j] = t;
+            sum[j] = s;
+        }
+    }
+    // the two halves of a wavefront, then the two wavefronts with the same columns
+    float* shared = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float t2 = __shfl_xor(top[j], 32), s2 = __shfl_xor(sum[j], 32), t = fmaxf(top[j], t2);
+        sum[j] = sum[j] * exp_of(top[j] - t) + s2 * exp_of(t2 - t);
+        top[j] = t;
+        if (wave_id() >= 2 && lane_id() < 32) {
+            shared[acc_col(j) * 2] = top[j];
+            shared[acc_col(j) * 2 + 1] = sum[j];
+        }
+    }
+    __syncthreads();
+    if (wave_id() < 2 && lane_id() < 32)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float t2 = shared[acc_col(j) * 2], s2 = shared[acc_col(j) * 2 + 1], t = fmaxf(top[j], t2);
+            const int64_t at = (int64_t)blockIdx.y * a.n_pad + n0 + acc_col(j);
+            a.part_max[at] = t;
+            a.part_sum[at] = sum[j] * exp_of(top[j] - t) + s2 * exp_of(t2 - t);
+        }
+}
+
+// lse and loss of the gathered rows, a wavefront each: parts joined, then the products with the labels' rows.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
+                                                        int64_t w_stride) {
+    const int64_t p = (int64_t)blockIdx.x * 4 + wave_id();
+    if (p >= (int64_t)a.header->n_live) return;
+    float top = -FLT_MAX, sum = 0.f;
+    for (int32_t g = lane_id(); g < a.groups; g += kWave) {
+        const float t2 = a.part_max[(int64_t)g * a.n_pad + p], s2 = a.part_sum[(int64_t)g * a.n_pad + p];
+        const float t = fmaxf(top, t2);
+        sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
+        top = t;
+    }
+    for (int s = 32; s > 0; s >>= 1) {
+        const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s), t = fmaxf(top, t2);
+        sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
+        top = t;
+    }
+    const float lse = top + logf(sum);
+    const int64_t row = a.row_of[p];
+    float met = 0.f;
+    for (int32_t j = 0; j < a.k; ++j) {
+        const int32_t v = a.labels[row * a.k + j];
+        if (v < 0 || (int64_t)v >= a.V) continue;
+        float dot = 0.f;
+        for (int32_t e = lane_id(); e < a.d; e += kWave)
+            dot = fmaf((float)rows[p * a.dp + e], (float)w[(int64_t)v * w_stride + e], dot);
+        for (int s = 32; s > 0; s >>= 1) dot += __shfl_xor(dot, s);
+        met += dot;
+    }
+    if (lane_id() == 0) {
+        a.place_lse[p] = lse;
+        a.lse[row] = lse;
+        a.loss[row] = a.count[p] * lse - met;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ gradient
+// g (c p - count) of 128 vertices of the piece from v_first on and 128 rows, as [vertex][row].
+template <typename T>
+__global__ __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
+                                                         T* __restrict__ probs) {
+    __shared__ __align__(16) char lds[4 * kTileBytes];
+    constexpr int kPitch = kTile + 4;
+    const int64_t n0 = (int64_t)blockIdx.x * kTile, v0 = v_first + (int64_t)blockIdx.y * kTile;
+    if (n0 >= (int64_t)a.header->n_live) return;
+    Acc acc[2][2];
+    product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
+    // how often a vertex is among a row's labels: a lane owns a row's 128 counts
+    uint8_t* counts = reinterpret_cast<uint8_t*>(lds);
+    if (threadIdx.x < kTile) {
+        uint32_t* mine = reinterpret_cast<uint32_t*>(counts + threadIdx.x * kPitch);
+        for (int e = 0; e < kTile / 4; ++e) mine[e] = 0;
+        const int32_t row = a.row_of[n0 + threadIdx.x];
+        if (row >= 0)
+            for (int32_t j = 0; j < a.k; ++j) {
+                const int64_t at = (int64_t)a.labels[(int64_t)row * a.k + j] - v0;
+                if (at >= 0 && at < kTile && v0 + at < a.V) counts[threadIdx.x * kPitch + at]++;
+            }
+    }
+    __syncthreads();
+    const float scale = a.header->scale;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int col = acc_col(j);
+        const float lse = a.place_lse[n0 + col], c = a.count[n0 + col], g = a.weight[n0 + col] * scale;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = acc_row(i, r);
+                const float held = (float)counts[col * kPitch + row];
+                const float p = v0 + row < a.V && c > 0.f ? g * (c * exp_of(acc[i][j][r] - lse) - held) : 0.f;
+                probs[((int64_t)blockIdx.y * kTile + row) * a.n_pad + n0 + col] = (T)p;
+            }
+    }
+}
+
+// dw of 128 vertices of the piece and 128 numbers of their rows.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
+                                                      T* __restrict__ dw, int64_t dw_stride) {
+    __shared__ __align__(16) char lds[4 * kTileBytes];
+    const int64_t m0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTile;
+    const int64_t live = a.header->n_live, k1 = (live + Kind<T>::kStep - 1) / Kind<T>::kStep * Kind<T>::kStep;
+    Acc acc[2][2];
+    product<T, false, true>(probs, x, m0, d0, 0, k1, lds, acc);
+    const float back = 1.f / a.header->scale;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int64_t v = v_first + m0 + acc_row(i, r), e = d0 + acc_col(j);
+                if (v < a.V && e < a.d) dw[v * dw_stride + e] = (T)(acc[i][j][r] * back);
+            }
+}
+
+// dx of 128 rows and 128 numbers, summed over a share of the piece's vertices.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
+                                                      int64_t v_share, int64_t v_end, int first_piece,
+                                                      float* __restrict__ parts) {
+    __shared__ __align__(16) char lds[4 * kTileBytes];
+    const int64_t n0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTile;
+    if (n0 >= (int64_t)a.header->n_live) return;
+    const int64_t k0 = (int64_t)blockIdx.z * v_share;
+    const int64_t k1 = k0 + v_share < v_end ? k0 + v_share : v_end;
+    Operand<T> piece = w;
+    piece.base += v_first * w.stride;
+    piece.rows -= v_first;
+    Acc acc[2][2];
+    product<T, true, true>(probs, piece, n0, d0, k0, k1, lds, acc);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int64_t e = d0 + acc_col(j);
+                if (e >= a.dp) continue;
+                float* at = parts + ((int64_t)blockIdx.z * a.n_pad + n0 + acc_row(i, r)) * a.dp + e;
+                *at = first_piece ? acc[i][j][r] : *at + acc[i][j][r];
+            }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dx_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
+                                                           T* __restrict__ dx, int64_t dx_stride) {
+    const int64_t p = (int64_t)blockIdx.x * 4 + wave_id();
+    if (p >= (int64_t)a.header->n_live) return;
+    const float back = 1.f / a.header->scale;
+    const int64_t row = a.row_of[p];
+    for (int32_t e = lane_id(); e < a.d; e += kWave) {
+        float sum = 0.f;
+        for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * a.n_pad + p) * a.dp + e];
+        dx[row * dx_stride + e] = (T)(sum * back);
+    }
+}
+
+// --------------------------------------------------------------------------------------------------------- layout
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+struct LossPlan {
+    int64_t n_pad, blocks, piece;   // piece: vertices at a time (a multiple of a tile)
+    int32_t dp, groups, shares;
+    size_t o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, total;
+};
+LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int dtype, bool grad) {
+    LossPlan p{};
+    const int64_t b = (int64_t)dtype_bytes(dtype), step = 128 / b;
+    p.dp = (int32_t)((d + step - 1) / step * step);
+    p.blocks = n > 0 ? (n + kTile - 1) / kTile : 1;  // without rows: the header is written all the same
+    p.n_pad = p.blocks * kTile;
+    const int64_t v_tiles = (V + kTile - 1) / kTile;
+    // enough workgroups to fill the chip several times over
+    const int64_t groups = (1024 + p.blocks - 1) / p.blocks;
+    p.groups = (int32_t)(groups < v_tiles ? groups : v_tiles);
+    int64_t piece_tiles = (int64_t)(kPieceBytes / (size_t)(p.n_pad * kTile * b));
+    if (piece_tiles < 1) piece_tiles = 1;
+    if (piece_tiles > 32768) piece_tiles = 32768;
+    if (piece_tiles > v_tiles) piece_tiles = v_tiles;
+    p.piece = piece_tiles * kTile;
+    const int64_t dx_tiles = p.blocks * ((p.dp + kTile - 1) / kTile);
+    int64_t shares = (512 + dx_tiles - 1) / dx_tiles;
+    if (shares > 16) shares = 16;
+    if (shares > piece_tiles) shares = piece_tiles;
+    p.shares = (int32_t)shares;
+    size_t o = sizeof(LossHeader);
+    auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o += up256(bytes);
+        return at;
+    };
+    p.o_live = take((size_t)p.blocks * 4);
+    p.o_weight = take((size_t)p.blocks * 4);
+    p.o_bad = take((size_t)p.blocks * 4);
+    p.o_row = take((size_t)p.n_pad * 4);
+    p.o_count = take((size_t)p.n_pad * 4);
+    p.o_gweight = take((size_t)p.n_pad * 4);
+    p.o_lse = take((size_t)p.n_pad * 4);
+    p.o_max = take((size_t)p.groups * (size_t)p.n_pad * 4);
+    p.o_sum = take((size_t)p.groups * (size_t)p.n_pad * 4);
+    p.o_rows = take((size_t)p.n_pad * (size_t)p.dp * (size_t)b);
+    p.o_w = take((size_t)V * (size_t)p.dp * (size_t)b);
+    if (grad) {
+        p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
+        p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
+    }
+    p.total = o;
+    return p;
+}
+
+int check_loss_sizes(int64_t n, int64_t V, int32_t d, int32_t k, int dtype) {
+    int rc = check_row_type(dtype, d);
+    if (rc != ND_OK) return rc;
+    if (n < 0 || V < 1 || k < 1) {
+        set_error("n must not be negative, V and k at least 1");
+        return ND_ERR_BAD_ARGUMENT;
+    }
+    if (n >= (1ll << 30) || V >= (1ll << 31) || k > ND_MAX_LABELS || n * (int64_t)k >= (1ll << 31)) {
+        set_error("fewer than 2^30 rows, 2^31 vertices and 2^31 labels, at most %d labels per row", ND_MAX_LABELS);
+        return ND_ERR_TOO_LARGE;
+    }
+    return ND_OK;
+}
+
+struct LossCall {
+    const void *x, *w;
+    int64_t x_stride, w_stride;
+    int dtype;
+    int64_t n, V;
+    int32_t d, k;
+    const int32_t* labels;
+    const float* row_weight;
+    float *loss, *lse;
+    void *dx, *dw;
+    int64_t dx_stride, dw_stride;
+    bool grad;
+};
+
+template <typename T>
+int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream) {
+    LossArgs a{};
+    a.n = c.n;
+    a.V = c.V;
+    a.n_pad = p.n_pad;
+    a.d = c.d;
+    a.dp = p.dp;
+    a.k = c.k;
+    a.labels = c.labels;
+    a.row_weight = c.row_weight;
+    a.loss = c.loss;
+    a.lse = c.lse;
+    a.header = (LossHeader*)ws;
+    a.block_live = (uint32_t*)(ws + p.o_live);
+    a.block_weight = (float*)(ws + p.o_weight);
+    a.block_bad = (uint32_t*)(ws + p.o_bad);
+    a.row_of = (int32_t*)(ws + p.o_row);
+    a.count = (float*)(ws + p.o_count);
+    a.weight = (float*)(ws + p.o_gweight);
+    a.place_lse = (float*)(ws + p.o_lse);
+    a.part_max = (float*)(ws + p.o_max);
+    a.part_sum = (float*)(ws + p.o_sum);
+    a.groups = p.groups;
+    T* rows = (T*)(ws + p.o_rows);
+    const unsigned blocks = (unsigned)p.blocks;
+    hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kTile), 0, stream, a);
+    hipLaunchKernelGGL(gather_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, a, (const T*)c.x, c.x_stride, rows,
+                       c.grad ? (T*)c.dx : nullptr, c.dx_stride, (int32_t)blocks);
+    const T* w = (const T*)c.w;
+    int64_t w_stride = c.w_stride;
+    const bool as_it_is = c.d == p.dp && w_stride * (int64_t)sizeof(T) % kChunk == 0 && (uintptr_t)w % kChunk == 0;
+    if (!as_it_is) {
+        T* padded = (T*)(ws + p.o_w);
+        const int64_t quads = (c.V + 3) / 4;
+        hipLaunchKernelGGL(pad_kernel<T>, dim3((unsigned)(quads < 16384 ? quads : 16384)), dim3(kThreads), 0, stream, w,
+                           w_stride, c.V, c.d, p.dp, padded);
+        w = padded;
+        w_stride = p.dp;
+    }
+    const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
+    if (c.n > 0) {
+        hipLaunchKernelGGL(stats_kernel<T>, dim3(blocks, (unsigned)p.groups), dim3(kThreads), 0, stream, a, ow, ox);
+        hipLaunchKernelGGL(loss_kernel<T>, dim3((unsigned)((c.n + 3) / 4)), dim3(kThreads), 0, stream, a, rows, w, w_stride);
+    }
+    if (c.grad) {
+        T* probs = (T*)(ws + p.o_probs);
+        float* parts = (float*)(ws + p.o_parts);
+        const unsigned d_tiles = (unsigned)((p.dp + kTile - 1) / kTile);
+        for (int64_t v = 0; v < c.V; v += p.piece) {
+            const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTile - 1) / kTile;
+            const Operand<T> op{probs, p.n_pad, tiles * kTile, (int32_t)p.n_pad};
+            if (c.n > 0)
+                hipLaunchKernelGGL(probs_kernel<T>, dim3(blocks, (unsigned)tiles), dim3(kThreads), 0, stream, a, ow, ox, v, probs);
+            if (c.dw)
+                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)tiles, d_tiles), dim3(kThreads), 0, stream, a, op, ox, v,
+                                   (T*)c.dw, c.dw_stride);
+            if (c.dx && c.n > 0) {
+                const int64_t share = (tiles + p.shares - 1) / p.shares * kTile;
+                hipLaunchKernelGGL(dx_kernel<T>, dim3(blocks, d_tiles, (unsigned)p.shares), dim3(kThreads), 0, stream, a, op, ow,
+                                   v, share, tiles * kTile, (int)(v == 0), parts);
+            }
+        }
+        if (c.dx && c.n > 0)
+            hipLaunchKernelGGL(dx_join_kernel<T>, dim3((unsigned)((c.n + 3) / 4)), dim3(kThreads), 0, stream, a, parts, p.shares,
+                               (T*)c.dx, c.dx_stride);
+    }
+    ND_HIP_CHECK(hipGetLastError());
+    return ND_OK;
+}
+
+int softmax_loss(const LossCall& c, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_loss_sizes(c.n, c.V, c.d, c.k, c.dtype);
+    if (rc == ND_OK) rc = check_rows("x_dev", c.x, c.n, c.d, c.x_stride, c.dtype);
+    if (rc == ND_OK) rc = check_rows("w_dev", c.w, c.V, c.d, c.w_stride, c.dtype);
+    if (rc == ND_OK && c.dx) rc = check_rows("dx_dev", c.dx, c.n, c.d, c.dx_stride, c.dtype);
+    if (rc == ND_OK && c.dw) rc = check_rows("dw_dev", c.dw, c.V, c.d, c.dw_stride, c.dtype);
+    if (rc != ND_OK) return rc;
+    if (!workspace || (c.n > 0 && (!c.labels || !c.loss || !c.lse))) {
+        set_error("a required pointer is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    const LossPlan p = plan_loss(c.n, c.V, c.d, c.dtype, c.grad);
+    if (workspace_bytes < p.total || ((uintptr_t)workspace % 256) != 0) {
+        set_error("workspace needs %zu bytes aligned to 256", p.total);
+        return ND_ERR_WORKSPACE;
+    }
+    switch (c.dtype) {
+        case ND_F32: return run_loss<float>(c, p, (char*)workspace, stream);
+        case ND_BF16: return run_loss<bf16_t>(c, p, (char*)workspace, stream);
+        default: return run_loss<f16_t>(c, p, (char*)workspace, stream);
+    }
+}
+
+}  // namespace
+}  // namespace nd
+
+using namespace nd;
+
+extern "C" {
+
+size_t nd_softmax_loss_workspace_bytes(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, int grad) {
+    if (check_loss_sizes(n, V, d, k, dtype) != ND_OK) return 0;
+    return plan_loss(n, V, d, dtype, grad != 0).total;
+}
+
+int nd_softmax_loss(const void* x_dev, int64_t x_stride, const void* w_dev, int64_t w_stride, int dtype, int64_t n,
+                    int64_t V, int32_t d, const int32_t* labels_dev, int32_t k, float* loss_dev, float* lse_dev,
+                    void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const LossCall c{x_dev, w_dev, x_stride, w_stride, dtype, n, V, d, k, labels_dev, nullptr, loss_dev, lse_dev,
+                     nullptr, nullptr, 0, 0, false};
+    return softmax_loss(c, workspace_dev, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int nd_softmax_loss_grad(const void* x_dev, int64_t x_stride, const void* w_dev, int64_t w_stride, int dtype, int64_t n,
+                         int64_t V, int32_t d, const int32_t* labels_dev, int32_t k, const float* row_weight_dev,
+                         float* loss_dev, float* lse_dev, void* dx_dev, int64_t dx_stride, void* dw_dev,
+                         int64_t dw_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const LossCall c{x_dev, w_dev, x_stride, w_stride, dtype, n, V, d, k, labels_dev, row_weight_dev, loss_dev, lse_dev,
+                     dx_dev, dw_dev, dx_stride, dw_stride, true};
+    return softmax_loss(c, workspace_dev, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int nd_softmax_loss_status(const void* workspace_dev, void* hip_stream) {
+    if (!workspace_dev) {
+        set_error("workspace is NULL");
+        return ND_ERR_NULL_POINTER;
+    }
+    uint32_t word = 0;
+    ND_HIP_CHECK(hipMemcpyAsync(&word, workspace_dev, 4, hipMemcpyDeviceToHost, (hipStream_t)hip_stream));
+    ND_HIP_CHECK(hipStreamSynchronize((hipStream_t)hip_stream));
+    if (word & 1u) {
+        set_error("a label was V or more; it was treated as NULL");
+        return ND_ERR_BAD_ROOT;
+    }
+    return ND_OK;
+}
+
+}  // extern "C"
