@@ -10,7 +10,7 @@
 #include <cfloat>
 #include <type_traits>
 
-#include "nd_rowtypes.h"
+#include "nd_sweep.h"
 #include "nd_wave.h"
 
 namespace nd {
@@ -24,33 +24,6 @@ constexpr size_t kPieceBytes = 512u << 20;  // probabilities that lie in the wor
 
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef short Short4 __attribute__((ext_vector_type(4)));
-
-struct LossHeader {
-    uint32_t status;   // bit 0: a label was V or more
-    uint32_t n_live;   // rows with labels
-    float scale;       // what probabilities are multiplied by before they are rounded, a power of two
-    uint32_t pad[61];
-};
-static_assert(sizeof(LossHeader) == 256, "one 256-byte block");
-
-// What the kernels share.  Arrays by place are those of the gathered rows.
-struct LossArgs {
-    int64_t n, V, n_pad;
-    int32_t d, dp, k;
-    const int32_t* labels;
-    const float* row_weight;
-    float *loss, *lse;        // by row
-    LossHeader* header;
-    uint32_t* block_live;     // per kTile rows: rows with labels,
-    float* block_weight;      // the largest weight among them,
-    uint32_t* block_bad;      // whether a label is V or more
-    int32_t* row_of;          // by place: row
-    float* count;             // by place: labels that count
-    float* weight;            // by place: row weight
-    float* place_lse;         // by place
-    float *part_max, *part_sum;  // [groups of vertices][n_pad]
-    int32_t groups;
-};
 
 __device__ __forceinline__ int32_t labels_of_row(const LossArgs& a, int64_t row, bool* bad) {
     int32_t c = 0;
@@ -147,6 +120,10 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* _
             a.row_of[before + at] = (int32_t)row;
             a.count[before + at] = (float)c;
             a.weight[before + at] = a.row_weight ? a.row_weight[row] : 1.f;
+            for (int32_t j = 0; j < a.k; ++j) {
+                const int32_t v = a.labels[row * a.k + j];
+                a.labels_of[(int64_t)(before + at) * a.k + j] = v >= 0 && (int64_t)v < a.V ? v : -1;
+            }
         } else if (row < a.n) {
             a.loss[row] = 0.f;
             a.lse[row] = 0.f;
@@ -175,6 +152,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* _
             a.count[p] = 0.f;
             a.weight[p] = 0.f;
             a.place_lse[p] = 0.f;
+            for (int32_t j = 0; j < a.k; ++j) a.labels_of[(int64_t)p * a.k + j] = -1;
         }
         for (int64_t e = (int64_t)all * a.dp + threadIdx.x; e < (int64_t)padded * a.dp; e += kThreads) rows[e] = (T)0.f;
     }
@@ -401,36 +379,37 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                         int64_t w_stride) {
-    const int64_t p = (int64_t)blockIdx.x * 4 + wave_id();
-    if (p >= (int64_t)a.header->n_live) return;
-    float top = -FLT_MAX, sum = 0.f;
-    for (int32_t g = lane_id(); g < a.groups; g += kWave) {
-        const float t2 = a.part_max[(int64_t)g * a.n_pad + p], s2 = a.part_sum[(int64_t)g * a.n_pad + p];
-        const float t = fmaxf(top, t2);
-        sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
-        top = t;
-    }
-    for (int s = 32; s > 0; s >>= 1) {
-        const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s), t = fmaxf(top, t2);
-        sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
-        top = t;
-    }
-    const float lse = top + logf(sum);
-    const int64_t row = a.row_of[p];
-    float met = 0.f;
-    for (int32_t j = 0; j < a.k; ++j) {
-        const int32_t v = a.labels[row * a.k + j];
-        if (v < 0 || (int64_t)v >= a.V) continue;
-        float dot = 0.f;
-        for (int32_t e = lane_id(); e < a.d; e += kWave)
-            dot = fmaf((float)rows[p * a.dp + e], (float)w[(int64_t)v * w_stride + e], dot);
-        for (int s = 32; s > 0; s >>= 1) dot += __shfl_xor(dot, s);
-        met += dot;
-    }
-    if (lane_id() == 0) {
-        a.place_lse[p] = lse;
-        a.lse[row] = lse;
-        a.loss[row] = a.count[p] * lse - met;
+    const int64_t live = a.header->n_live;
+    for (int64_t p = (int64_t)blockIdx.x * 4 + wave_id(); p < live; p += (int64_t)gridDim.x * 4) {
+        float top = -FLT_MAX, sum = 0.f;
+        for (int32_t g = lane_id(); g < a.groups; g += kWave) {
+            const float t2 = a.part_max[(int64_t)g * a.n_pad + p], s2 = a.part_sum[(int64_t)g * a.n_pad + p];
+            const float t = fmaxf(top, t2);
+            sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
+            top = t;
+        }
+        for (int s = 32; s > 0; s >>= 1) {
+            const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s), t = fmaxf(top, t2);
+            sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
+            top = t;
+        }
+        const float lse = top + logf(sum);
+        const int64_t row = a.row_of[p];
+        float met = 0.f;
+        for (int32_t j = 0; j < a.k; ++j) {
+            const int32_t v = a.labels_of[p * a.k + j];
+            if (v < 0) continue;
+            float dot = 0.f;
+            for (int32_t e = lane_id(); e < a.d; e += kWave)
+                dot = fmaf((float)rows[p * a.dp + e], (float)w[(int64_t)v * w_stride + e], dot);
+            for (int s = 32; s > 0; s >>= 1) dot += __shfl_xor(dot, s);
+            met += dot;
+        }
+        if (lane_id() == 0) {
+            a.place_lse[p] = lse;
+            a.lse[row] = lse;
+            a.loss[row] = a.count[p] * lse - met;
+        }
     }
 }
 
@@ -450,12 +429,10 @@ __global__ __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> 
     if (threadIdx.x < kTile) {
         uint32_t* mine = reinterpret_cast<uint32_t*>(counts + threadIdx.x * kPitch);
         for (int e = 0; e < kTile / 4; ++e) mine[e] = 0;
-        const int32_t row = a.row_of[n0 + threadIdx.x];
-        if (row >= 0)
-            for (int32_t j = 0; j < a.k; ++j) {
-                const int64_t at = (int64_t)a.labels[(int64_t)row * a.k + j] - v0;
-                if (at >= 0 && at < kTile && v0 + at < a.V) counts[threadIdx.x * kPitch + at]++;
-            }
+        for (int32_t j = 0; j < a.k; ++j) {
+            const int64_t v = a.labels_of[(n0 + threadIdx.x) * a.k + j];
+            if (v >= v0 && v < v0 + kTile) counts[threadIdx.x * kPitch + (v - v0)]++;
+        }
     }
     __syncthreads();
     const float scale = a.header->scale;
@@ -527,29 +504,37 @@ __global__ __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> pro
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dx_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
                                                            T* __restrict__ dx, int64_t dx_stride) {
-    const int64_t p = (int64_t)blockIdx.x * 4 + wave_id();
-    if (p >= (int64_t)a.header->n_live) return;
-    const float back = 1.f / a.header->scale;
-    const int64_t row = a.row_of[p];
-    for (int32_t e = lane_id(); e < a.d; e += kWave) {
-        float sum = 0.f;
-        for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * a.n_pad + p) * a.dp + e];
-        dx[row * dx_stride + e] = (T)(sum * back);
+    const int64_t live = a.header->n_live;
+    for (int64_t p = (int64_t)blockIdx.x * 4 + wave_id(); p < live; p += (int64_t)gridDim.x * 4) {
+        const float back = 1.f / a.header->scale;
+        const int64_t row = a.row_of[p];
+        for (int32_t e = lane_id(); e < a.d; e += kWave) {
+            float sum = 0.f;
+            for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * a.n_pad + p) * a.dp + e];
+            dx[row * dx_stride + e] = (T)(sum * back);
+        }
     }
 }
 
 // --------------------------------------------------------------------------------------------------------- layout
+// A launch holds fewer than 2^32 lanes: wavefronts go on to further rows from here on.
+inline dim3 wave_per(int64_t rows) {
+    const int64_t groups = (rows + 3) / 4;
+    return dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20));
+}
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct LossPlan {
     int64_t n_pad, blocks, piece;   // piece: vertices at a time (a multiple of a tile)
     int32_t dp, groups, shares;
-    size_t o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, total;
+    bool sweep;                     // rows short enough for nd_sweep.hip
+    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, total;
 };
-LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int dtype, bool grad) {
+LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool grad) {
     LossPlan p{};
     const int64_t b = (int64_t)dtype_bytes(dtype), step = 128 / b;
-    p.dp = (int32_t)((d + step - 1) / step * step);
+    p.sweep = dtype != ND_F32 && sweep_width(d) > 0;
+    p.dp = p.sweep ? sweep_width(d) : (int32_t)((d + step - 1) / step * step);
     p.blocks = n > 0 ? (n + kTile - 1) / kTile : 1;  // without rows: the header is written all the same
     p.n_pad = p.blocks * kTile;
     const int64_t v_tiles = (V + kTile - 1) / kTile;
@@ -579,10 +564,25 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int dtype, bool grad) {
     p.o_count = take((size_t)p.n_pad * 4);
     p.o_gweight = take((size_t)p.n_pad * 4);
     p.o_lse = take((size_t)p.n_pad * 4);
-    p.o_max = take((size_t)p.groups * (size_t)p.n_pad * 4);
-    p.o_sum = take((size_t)p.groups * (size_t)p.n_pad * 4);
+    p.o_labels = take((size_t)p.n_pad * (size_t)k * 4);
     p.o_rows = take((size_t)p.n_pad * (size_t)p.dp * (size_t)b);
     p.o_w = take((size_t)V * (size_t)p.dp * (size_t)b);
+    if (p.sweep) {
+        // the sweeps run one after the other and share the segments' memory
+        size_t held = 0, sums = 0;
+        for (int mode = kSweepLse; mode <= (grad ? kSweepDw : kSweepLse); ++mode) {
+            const size_t rows = (size_t)sweep_segments(mode, mode == kSweepDw ? V : n, p.dp) * (size_t)sweep_held(mode, p.dp);
+            if (rows > held) held = rows;
+            if (mode != kSweepLse && rows > sums) sums = rows;
+        }
+        p.o_max = take(held * 4);
+        p.o_sum = take(held * 4);
+        p.o_parts = take(sums * (size_t)p.dp * 4);
+        p.total = o;
+        return p;
+    }
+    p.o_max = take((size_t)p.groups * (size_t)p.n_pad * 4);
+    p.o_sum = take((size_t)p.groups * (size_t)p.n_pad * 4);
     if (grad) {
         p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
         p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
@@ -643,6 +643,8 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     a.part_max = (float*)(ws + p.o_max);
     a.part_sum = (float*)(ws + p.o_sum);
     a.groups = p.groups;
+    a.labels_of = (int32_t*)(ws + p.o_labels);
+    a.div_k = make_fastdiv((uint32_t)c.k);
     T* rows = (T*)(ws + p.o_rows);
     const unsigned blocks = (unsigned)p.blocks;
     hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kTile), 0, stream, a);
@@ -659,10 +661,22 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         w = padded;
         w_stride = p.dp;
     }
+    if constexpr (sizeof(T) == 2)
+        if (p.sweep) {
+            const SweepParts parts{a.part_max, a.part_sum, (float*)(ws + p.o_parts)};
+            const int mode = c.grad && c.dx ? kSweepDx : kSweepLse;
+            int rc = ND_OK;
+            if (c.n > 0) {
+                rc = sweep<T>(mode, a, rows, w, w_stride, parts, nullptr, 0, stream);
+                if (rc == ND_OK) rc = sweep_finish<T>(mode, a, rows, w, w_stride, parts, (T*)c.dx, c.dx_stride, stream);
+            }
+            if (rc == ND_OK && c.grad && c.dw) rc = sweep<T>(kSweepDw, a, rows, w, w_stride, parts, (T*)c.dw, c.dw_stride, stream);
+            return rc;
+        }
     const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
     if (c.n > 0) {
         hipLaunchKernelGGL(stats_kernel<T>, dim3(blocks, (unsigned)p.groups), dim3(kThreads), 0, stream, a, ow, ox);
-        hipLaunchKernelGGL(loss_kernel<T>, dim3((unsigned)((c.n + 3) / 4)), dim3(kThreads), 0, stream, a, rows, w, w_stride);
+        hipLaunchKernelGGL(loss_kernel<T>, wave_per(c.n), dim3(kThreads), 0, stream, a, rows, w, w_stride);
     }
     if (c.grad) {
         T* probs = (T*)(ws + p.o_probs);
@@ -683,7 +697,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
             }
         }
         if (c.dx && c.n > 0)
-            hipLaunchKernelGGL(dx_join_kernel<T>, dim3((unsigned)((c.n + 3) / 4)), dim3(kThreads), 0, stream, a, parts, p.shares,
+            hipLaunchKernelGGL(dx_join_kernel<T>, wave_per(c.n), dim3(kThreads), 0, stream, a, parts, p.shares,
                                (T*)c.dx, c.dx_stride);
     }
     ND_HIP_CHECK(hipGetLastError());
@@ -701,7 +715,7 @@ int softmax_loss(const LossCall& c, void* workspace, size_t workspace_bytes, hip
         set_error("a required pointer is NULL");
         return ND_ERR_NULL_POINTER;
     }
-    const LossPlan p = plan_loss(c.n, c.V, c.d, c.dtype, c.grad);
+    const LossPlan p = plan_loss(c.n, c.V, c.d, c.k, c.dtype, c.grad);
     if (workspace_bytes < p.total || ((uintptr_t)workspace % 256) != 0) {
         set_error("workspace needs %zu bytes aligned to 256", p.total);
         return ND_ERR_WORKSPACE;
@@ -722,7 +736,7 @@ extern "C" {
 
 size_t nd_softmax_loss_workspace_bytes(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, int grad) {
     if (check_loss_sizes(n, V, d, k, dtype) != ND_OK) return 0;
-    return plan_loss(n, V, d, dtype, grad != 0).total;
+    return plan_loss(n, V, d, k, dtype, grad != 0).total;
 }
 
 int nd_softmax_loss(const void* x_dev, int64_t x_stride, const void* w_dev, int64_t w_stride, int dtype, int64_t n,

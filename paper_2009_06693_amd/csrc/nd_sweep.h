@@ -1,0 +1,88 @@
+// Rows held in registers against rows that pass by in LDS: the softmax loss for rows of at most 256 numbers of a 16-bit
+// type, logits and the product that follows them in one kernel, so that no logit and no probability reaches memory.
+#pragma once
+
+#include "nd_rowtypes.h"
+
+namespace nd {
+
+constexpr int kSweepUnit = 64;      // passing rows at a time
+constexpr int kSweepGroups = 256;   // workgroups: one per compute unit
+constexpr int kSweepLeast = 4;      // units that a workgroup takes at least
+
+enum SweepMode {
+    kSweepLse = 0,   // x held, w passes: maximum and sum of exponentials per row of x
+    kSweepDx = 1,    // the same, and the sums of w's rows weighted with the exponentials
+    kSweepDw = 2,    // w held, x passes: sums of x's rows weighted with g (c p - count)
+};
+
+// How the work, tiles of held rows x units of passing rows, is dealt out: workgroup g takes the units
+// [g total / groups, (g + 1) total / groups) of all tiles in a row, so that every one has as many, whatever the number of
+// tiles; what it holds of a tile is a segment.
+struct SweepDeal {
+    int64_t tiles, units, total, groups;
+    __host__ __device__ SweepDeal(int64_t held, int held_tile, int64_t passing) {
+        tiles = (held + held_tile - 1) / held_tile;
+        units = (passing + kSweepUnit - 1) / kSweepUnit;
+        total = tiles * units;
+        groups = total / kSweepLeast;
+        if (groups > kSweepGroups) groups = kSweepGroups;
+        if (groups < 1) groups = 1;
+    }
+    __host__ __device__ int64_t first(int64_t g) const { return g * total / groups; }
+    // the workgroup that has unit x
+    __host__ __device__ int64_t group_of(int64_t x) const {
+        int64_t g = x * groups / total;
+        while (g + 1 < groups && first(g + 1) <= x) ++g;
+        while (g > 0 && first(g) > x) --g;
+        return g;
+    }
+};
+
+// What the kernels of the loss share.  Arrays by place are those of the gathered rows: the rows with labels, in their
+// order, one after the other.
+struct LossHeader {
+    uint32_t status;   // bit 0: a label was V or more
+    uint32_t n_live;   // rows with labels
+    float scale;       // what probabilities are multiplied by before they are rounded, a power of two
+    uint32_t pad[61];
+};
+static_assert(sizeof(LossHeader) == 256, "one 256-byte block");
+
+struct LossArgs {
+    int64_t n, V, n_pad;
+    int32_t d, dp, k;
+    const int32_t* labels;
+    const float* row_weight;
+    float *loss, *lse;        // by row
+    LossHeader* header;
+    uint32_t* block_live;     // per 128 rows: rows with labels,
+    float* block_weight;      // the largest weight among them,
+    uint32_t* block_bad;      // whether a label is V or more
+    int32_t* row_of;          // by place: row
+    int32_t* labels_of;       // by place: k labels, -1 where one does not count
+    float* count;             // by place: labels that count
+    float* weight;            // by place: row weight
+    float* place_lse;         // by place
+    float *part_max, *part_sum;  // [groups of vertices][n_pad]
+    int32_t groups;
+    FastDiv div_k;
+};
+
+// Memory of a sweep's segments.
+struct SweepParts {
+    float *top, *sum;   // [segment][held rows of a tile]
+    float* rows;        // [segment][held rows of a tile][dp]
+};
+int sweep_width(int32_t d);                   // numbers in a padded row, 0: rows are too long
+int sweep_held(int mode, int32_t dp);         // held rows of a tile
+int64_t sweep_segments(int mode, int64_t held, int32_t dp);
+template <typename T>
+int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stride, const SweepParts& parts, T* dw,
+          int64_t dw_stride, hipStream_t stream);
+// lse, loss and (dx: not null) dx of the gathered rows, from the segments of the sweep in `mode`.
+template <typename T>
+int sweep_finish(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stride, const SweepParts& parts, T* dx,
+                 int64_t dx_stride, hipStream_t stream);
+
+}  // namespace nd
