@@ -6,6 +6,7 @@
 
 namespace nd {
 
+constexpr int kSweepHeld = 256;     // held rows of a tile
 constexpr int kSweepUnit = 64;      // passing rows at a time
 constexpr int kSweepGroups = 256;   // workgroups: one per compute unit
 constexpr int kSweepLeast = 4;      // units that a workgroup takes at least
@@ -75,8 +76,7 @@ struct SweepParts {
     float* rows;        // [segment][held rows of a tile][dp]
 };
 int sweep_width(int32_t d);                   // numbers in a padded row, 0: rows are too long
-int sweep_held(int mode, int32_t dp);         // held rows of a tile
-int64_t sweep_segments(int mode, int64_t held, int32_t dp);
+int64_t sweep_segments(int mode, int64_t held);
 template <typename T>
 int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stride, const SweepParts& parts, T* dw,
           int64_t dw_stride, hipStream_t stream);

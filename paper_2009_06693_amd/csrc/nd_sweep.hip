@@ -18,7 +18,6 @@ namespace nd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRing = 4;           // units in LDS
 constexpr float kLog2e = 1.44269504088896340736f;
 
 typedef float Acc __attribute__((ext_vector_type(16)));
@@ -39,17 +38,20 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 
 template <int MODE, int D>
 struct Shape {
-    // Held rows of a wavefront, in columns of 32.  What they take of the 512 registers: D / 8 for the rows, D / 2 for the
-    // sums, per column.
-    static constexpr int kColumns = MODE == kSweepLse || D <= 128 ? 2 : 1;
-    static constexpr int kHeld = 4 * 32 * kColumns;
+    static constexpr int kThreads = 512;               // two wavefronts per SIMD: one multiplies while the other takes exponentials
+    static constexpr int kHeld = kSweepHeld;           // 32 held rows per wavefront
+    // A block's scores are made while the block before is still being worked on, where there are registers for both
+    // (of 256: D / 8 for the held rows, D / 2 for the sums, 16 + 8 per block under way).
+    static constexpr bool kAhead = D <= 128;
+    static constexpr int kRing = kAhead ? 4 : 2;       // units in LDS
     static constexpr int kSteps = D / 16;              // instructions along a row
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
     static constexpr int kUnitBytes = kSweepUnit * D * 2;
     static constexpr int kLoads = kUnitBytes / (kThreads * 16);  // pieces that a lane moves per unit
-    // kSweepDw: counts of labels, a byte per (held row, passing row) of a unit, for two units
+    // kSweepDw: what the passing rows weigh, and counts of labels, a byte per (held row, passing row) of a unit, two units
+    static constexpr int kFactorBytes = MODE == kSweepDw ? 3 * kSweepUnit * 4 : 0;
     static constexpr int kCountBytes = MODE == kSweepDw ? kHeld * kSweepUnit : 0;
-    static constexpr int kLds = kRing * kUnitBytes + 2 * kCountBytes + (MODE == kSweepDw ? 64 : 0);
+    static constexpr int kLds = kRing * (kUnitBytes + kFactorBytes) + 2 * kCountBytes + (MODE == kSweepDw ? 64 : 0);
 };
 
 // Byte position of piece c of row r of a unit: pieces change places so that 16 rows' reads of one piece, and 4 rows' reads of
@@ -60,6 +62,16 @@ __device__ __forceinline__ int place(int r, int c) {
     return (r * (D / 8) + (c ^ (((r & 3) << 2) | ((r >> 2) & 3)))) * 16;
 }
 
+// A barrier for what lies in LDS only: loads from memory stay under way across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <typename V>
+using LdsOf = __attribute__((address_space(3))) V;
+
 struct SweepArgs {
     const void *held, *passing;
     int64_t held_stride, passing_stride;
@@ -69,16 +81,16 @@ struct SweepArgs {
 };
 
 template <typename T, int D, int MODE>
-__global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kThreads) void sweep_kernel(LossArgs a, SweepArgs s) {
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) void sweep_kernel(LossArgs a, SweepArgs s) {
     using Sh = Shape<MODE, D>;
     using V8 = typename Eight<T>::V;
-    constexpr int COLS = Sh::kColumns, HELD = Sh::kHeld, STEPS = Sh::kSteps;
-    constexpr bool kSums = MODE != kSweepLse, kOnline = MODE != kSweepDw;
+    constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing;
+    constexpr bool kSums = MODE != kSweepLse, kOnline = MODE != kSweepDw, kAhead = Sh::kAhead;
     // fp16 ends at 2^-24: exponentials are taken times 2^8 and may outgrow the maximum that they are relative to by 2^6
     constexpr float kRaise = std::is_same<T, f16_t>::value ? 8.f : 0.f;
-    constexpr float kSlack = 4.f;  // e^4 < 2^6
+    const uint32_t kMost = __float_as_uint(std::is_same<T, f16_t>::value ? 16384.f : 64.f);  // 2^6 times that
     extern __shared__ __align__(16) char lds[];
-    const int lane = lane_id(), wave = wave_id(), half = lane >> 5, col = lane & 31;
+    const int lane = lane_id(), wave = (int)wave_uniform((uint32_t)wave_id()), half = lane >> 5, col = lane & 31;
     const int64_t live = a.header->n_live;
     const int64_t held_rows = MODE == kSweepDw ? a.V : live, passing_rows = MODE == kSweepDw ? live : a.V;
     if (held_rows == 0 || passing_rows == 0) return;
@@ -86,312 +98,396 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kThreads
     if ((int64_t)blockIdx.x >= deal.groups) return;
     const T* held = (const T*)s.held;
     const T* passing = (const T*)s.passing;
-    uint8_t* counts = (uint8_t*)(lds + kRing * Sh::kUnitBytes);
-    uint32_t* touched = (uint32_t*)(lds + kRing * Sh::kUnitBytes + 2 * Sh::kCountBytes);  // a bit per (32 passing, 32 held)
+    float* factors = (float*)(lds + RING * Sh::kUnitBytes);                    // [unit][lse log2 e, g c, g][passing row]
+    char* counts = lds + RING * (Sh::kUnitBytes + Sh::kFactorBytes);           // [unit][held row][passing row]
+    uint32_t* touched = (uint32_t*)(counts + 2 * Sh::kCountBytes);             // [unit][wavefront]: a bit per block with counts
+    const float scale = MODE == kSweepDw ? a.header->scale : 1.f;
+
+    uint32_t load_at[Sh::kLoads];  // where a lane's pieces of a unit lie
+#pragma unroll
+    for (int i = 0; i < Sh::kLoads; ++i) {
+        const int e = i * THREADS + (int)threadIdx.x;
+        load_at[i] = (uint32_t)(e / Sh::kPieces) * (uint32_t)s.passing_stride + e % Sh::kPieces * 8;
+    }
+    // where a lane reads in a unit: pieces of a row (a block's 32 rows), and four rows of a column's 8 bytes (16 rows); what
+    // the kernel adds to them is known when it is compiled
+    typedef LdsOf<char> LdsChar;
+    LdsChar* unit_lds = (LdsChar*)lds;
+    int32_t score_at[STEPS < 8 ? STEPS : 8], column_at[2][D / 32 < 4 ? D / 32 : 4];
+#pragma unroll
+    for (int k = 0; k < (STEPS < 8 ? STEPS : 8); ++k) score_at[k] = place<D>(col, k * 2 + half);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int j = 0; j < (D / 32 < 4 ? D / 32 : 4); ++j) {
+            const int sub = lane & 15, at = j * 32 + ((lane >> 4) & 1) * 16 + (sub & 3) * 4;
+            column_at[e][j] = place<D>(e * 8 + half * 4 + (sub >> 2), at / 8) + (at & 4) * 2;
+        }
 
     const int64_t end = deal.first((int64_t)blockIdx.x + 1);
     for (int64_t x = deal.first(blockIdx.x); x < end;) {
         const int64_t tile = x / deal.units;
-        const int64_t u0 = x - tile * deal.units, u1 = end - x < deal.units - u0 ? u0 + (end - x) : deal.units;
-        const int64_t row0 = tile * HELD + wave * (32 * COLS);
+        const int32_t u0 = (int32_t)(x - tile * deal.units);
+        const int32_t u1 = (int32_t)(end - x < deal.units - u0 ? u0 + (end - x) : deal.units);
+        const int64_t row0 = tile * HELD + wave * 32;
         x += u1 - u0;
 
+        // ---- passing rows on their way to LDS
         uint4 ahead[Sh::kLoads];
-        auto load = [&](int64_t u) {
+        float factor_ahead[3];
+        auto load = [&](int32_t u) {
+            // gathered rows are padded with zeros to whole units, but no further
+            const int64_t r0 = (int64_t)u * kSweepUnit, last = (MODE == kSweepDw ? deal.units * kSweepUnit : passing_rows) - 1 - r0;
+            const T* from = passing + r0 * s.passing_stride;
+            if (last >= kSweepUnit - 1) {
 #pragma unroll
-            for (int i = 0; i < Sh::kLoads; ++i) {
-                const int e = i * kThreads + (int)threadIdx.x;
-                int64_t r = u * kSweepUnit + e / Sh::kPieces;
-                if (MODE != kSweepDw && r >= passing_rows) r = passing_rows - 1;  // gathered rows are padded
-                ahead[i] = *reinterpret_cast<const uint4*>(passing + r * s.passing_stride + e % Sh::kPieces * 8);
+                for (int i = 0; i < Sh::kLoads; ++i) ahead[i] = *reinterpret_cast<const uint4*>(from + load_at[i]);
+            } else {  // rows behind the last one are the last one again
+#pragma unroll
+                for (int i = 0; i < Sh::kLoads; ++i) {
+                    const int e = i * THREADS + (int)threadIdx.x;
+                    const int64_t r = e / Sh::kPieces < last ? e / Sh::kPieces : last;
+                    ahead[i] = *reinterpret_cast<const uint4*>(from + r * s.passing_stride + e % Sh::kPieces * 8);
+                }
+            }
+            if (MODE == kSweepDw && threadIdx.x < kSweepUnit) {
+                factor_ahead[0] = INFINITY;  // behind the segment's last unit nothing weighs
+                factor_ahead[1] = 0.f;
+                factor_ahead[2] = 0.f;
+                if (u < u1) {
+                    const int64_t p = r0 + threadIdx.x;
+                    const float g = a.weight[p] * scale;
+                    factor_ahead[0] = a.place_lse[p] * kLog2e;
+                    factor_ahead[1] = g * a.count[p];
+                    factor_ahead[2] = g;
+                }
             }
         };
         auto keep = [&](int slot) {
 #pragma unroll
             for (int i = 0; i < Sh::kLoads; ++i) {
-                const int e = i * kThreads + (int)threadIdx.x;
+                const int e = i * THREADS + (int)threadIdx.x;
                 *reinterpret_cast<uint4*>(lds + slot * Sh::kUnitBytes + place<D>(e / Sh::kPieces, e % Sh::kPieces)) = ahead[i];
             }
+            if (MODE == kSweepDw && threadIdx.x < kSweepUnit)
+#pragma unroll
+                for (int i = 0; i < 3; ++i) factors[(slot * 3 + i) * kSweepUnit + threadIdx.x] = factor_ahead[i];
         };
 
-        // held rows, as operands
-        V8 rows[COLS][STEPS];
+        // ---- labels of a unit's rows that are among the held ones
+        constexpr int kLabelLoads = MODE == kSweepDw ? 2 : 1;
+        const uint32_t unit_labels = (uint32_t)(kSweepUnit * a.k);
+        int32_t met[kLabelLoads];
+        auto load_labels = [&](int32_t u) {
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) {
-            int64_t r = row0 + c * 32 + col;
+            for (int i = 0; i < kLabelLoads; ++i) {
+                const uint32_t e = (uint32_t)(i * THREADS) + threadIdx.x;
+                met[i] = e < unit_labels ? a.labels_of[(int64_t)u * unit_labels + e] : -1;
+            }
+        };
+        const int64_t held0 = tile * HELD;
+        auto count_label = [&](int32_t v, uint32_t e, int buffer) {
+            const uint64_t h = (uint64_t)((int64_t)v - held0);
+            if (v < 0 || h >= (uint64_t)HELD) return;
+            const uint32_t r = fastdiv(e, a.div_k), at = (uint32_t)h * kSweepUnit + r;
+            atomicAdd((uint32_t*)(counts + buffer * Sh::kCountBytes + (at & ~3u)), 1u << (8u * (at & 3u)));
+            atomicOr(&touched[buffer * 8 + h / 32u], 1u << (r / 32u));
+        };
+        auto count_labels = [&](int32_t u, int buffer) {
+#pragma unroll
+            for (int i = 0; i < kLabelLoads; ++i) count_label(met[i], (uint32_t)(i * THREADS) + threadIdx.x, buffer);
+            for (uint32_t e = (uint32_t)(kLabelLoads * THREADS) + threadIdx.x; e < unit_labels; e += THREADS)
+                count_label(a.labels_of[(int64_t)u * unit_labels + e], e, buffer);
+        };
+
+        // ---- held rows, as operands
+        V8 rows[STEPS];
+        {
+            int64_t r = row0 + col;
             r = r < held_rows ? r : held_rows - 1;
 #pragma unroll
             for (int k = 0; k < STEPS; ++k)
-                rows[c][k] = *reinterpret_cast<const V8*>(held + r * s.held_stride + k * 16 + half * 8);
+                rows[k] = *reinterpret_cast<const V8*>(held + r * s.held_stride + k * 16 + half * 8);
         }
-        Acc sums[COLS][D / 32];
-        float top[COLS], top2[COLS], total[COLS];  // maximum, the same in the exponent of 2, sum
+        Acc sums[D / 32];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) {
-            top[c] = -FLT_MAX;
-            top2[c] = 0.f;
-            total[c] = 0.f;
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) sums[c][j] = Acc{};
-        }
+        for (int j = 0; j < D / 32; ++j) sums[j] = Acc{};
+        float top = -FLT_MAX, top2 = 0.f, total = 0.f;  // maximum, the same in the exponent of 2, sum
 
-        // labels of a unit's rows that are among the held ones
-        constexpr int kLabelLoads = MODE == kSweepDw ? 3 : 1;
-        const uint32_t unit_labels = (uint32_t)(kSweepUnit * a.k);
-        int32_t met[kLabelLoads];
-        auto load_labels = [&](int64_t u) {
-#pragma unroll
-            for (int i = 0; i < kLabelLoads; ++i) {
-                const uint32_t e = (uint32_t)(i * kThreads) + threadIdx.x;
-                met[i] = e < unit_labels ? a.labels_of[u * unit_labels + e] : -1;
-            }
-        };
-        auto count_label = [&](int32_t v, uint32_t e, int buffer) {
-            const int64_t h = (int64_t)v - tile * HELD;
-            if (v < 0 || h < 0 || h >= HELD) return;
-            const uint32_t r = fastdiv(e, a.div_k);
-            // [held row][passing row]
-            atomicAdd((uint32_t*)(counts + buffer * Sh::kCountBytes + (uint32_t)h * kSweepUnit + (r & ~3u)), 1u << (8u * (r & 3u)));
-            atomicOr(&touched[buffer], 1u << ((uint32_t)h / 32u * 2u + r / 32u));
-        };
-        auto count_labels = [&](int64_t u, int buffer) {
-#pragma unroll
-            for (int i = 0; i < kLabelLoads; ++i) count_label(met[i], (uint32_t)(i * kThreads) + threadIdx.x, buffer);
-            for (uint32_t e = (uint32_t)(kLabelLoads * kThreads) + threadIdx.x; e < unit_labels; e += kThreads)
-                count_label(a.labels_of[u * unit_labels + e], e, buffer);
-        };
-
-        __syncthreads();  // the segment before has read its units
+        lds_barrier();  // the segment before has read its units
         if (MODE == kSweepDw) {
-            for (int e = threadIdx.x * 16; e < 2 * Sh::kCountBytes; e += kThreads * 16)
+            for (int e = threadIdx.x * 16; e < 2 * Sh::kCountBytes; e += THREADS * 16)
                 *reinterpret_cast<uint4*>(counts + e) = uint4{0, 0, 0, 0};
-            if (threadIdx.x < 2) touched[threadIdx.x] = 0;
+            if (threadIdx.x < 16) touched[threadIdx.x] = 0;
+            load_labels(u0);
         }
+        if (kAhead)  // what the sums read in front of the first block
+            for (int e = threadIdx.x * 16; e < Sh::kUnitBytes; e += THREADS * 16)
+                *reinterpret_cast<uint4*>(lds + (RING - 1) * Sh::kUnitBytes + e) = uint4{0, 0, 0, 0};
         load(u0);
         keep(0);
-        if (u0 + 1 < u1) {
+        if (kAhead) {
             load(u0 + 1);
             keep(1);
         }
-        if (u0 + 2 < u1) load(u0 + 2);
-        if (MODE == kSweepDw) load_labels(u0);
-        __syncthreads();
+        load(u0 + (kAhead ? 2 : 1));
+        lds_barrier();
         if (MODE == kSweepDw) {
             count_labels(u0, 0);
             if (u0 + 1 < u1) load_labels(u0 + 1);
-            __syncthreads();
+            lds_barrier();
         }
 
-        // products of block b (0, 1) of the unit in `slot` with the held rows
-        auto scores = [&](Acc (&out)[COLS], int slot, int b) {
-            const char* from = lds + slot * Sh::kUnitBytes;
+        // ---- operands from LDS: a piece of 32 passing rows for the scores; 16 passing rows down 32 columns for the sums
+        auto row_piece = [&](int slot, int b, int k) {
+            return *reinterpret_cast<const LdsOf<V8>*>(unit_lds + score_at[k & 7] +
+                                                       (slot * Sh::kUnitBytes + b * 32 * D * 2 + (k >> 3) * 256));
+        };
+        auto column_piece = [&](int slot, int b, int i) {
+            const int t = i / (D / 32), j = i % (D / 32);
+            union {
+                V8 v;
+                Short4 q[2];
+            } p;
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) out[c] = Acc{};
+            for (int e = 0; e < 2; ++e)
+                p.q[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsOf<Short4>*>(
+                    unit_lds + column_at[e][j & 3] + (slot * Sh::kUnitBytes + (b * 32 + t * 16) * D * 2 + (j >> 2) * 256)));
+            return p.v;
+        };
+        // ---- scores of block b of the unit in `slot`
+        auto scores = [&](Acc& out, int slot, int b) {
+            out = Acc{};
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-                const V8 p = *reinterpret_cast<const V8*>(from + place<D>(b * 32 + col, k * 2 + half));
+            for (int k = 0; k < STEPS; ++k) out = multiply(row_piece(slot, b, k), rows[k], out);
+        };
+        // ---- sums += rows of the block, weighted
+        auto add_rows = [&](const V8 (&weight)[2], int slot, int b) {
 #pragma unroll
-                for (int c = 0; c < COLS; ++c) out[c] = multiply(p, rows[c][k], out[c]);
+            for (int i = 0; i < STEPS; ++i) {
+                const int t = i / (D / 32), j = i % (D / 32);
+                sums[j] = multiply(column_piece(slot, b, i), weight[t], sums[j]);
             }
         };
-        // sums += rows of the block, weighted
-        auto add_rows = [&](const V8 (&weight)[COLS][2], int slot, int b) {
-            const char* from = lds + slot * Sh::kUnitBytes;
-            const int sub = lane & 15, right = (lane >> 4) & 1;
+        // ---- both, for two blocks, an instruction of each in turn, and `share(i)`, a STEPS-th of other work, in
+        // between; operands are read two turns before they are used
+        auto scores_and_sums = [&](Acc& out, int slot, int b, const V8 (&weight)[2], int sum_slot, int sum_b, auto&& share) {
+            out = Acc{};
+            V8 r[3], c[3];
+            r[0] = row_piece(slot, b, 0);
+            if (kSums) c[0] = column_piece(sum_slot, sum_b, 0);
+            r[1] = row_piece(slot, b, 1);
+            if (kSums) c[1] = column_piece(sum_slot, sum_b, 1);
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    union {
-                        V8 v;
-                        Short4 q[2];
-                    } p;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = b * 32 + t * 16 + e * 8 + half * 4 + (sub >> 2), at = j * 32 + right * 16 + (sub & 3) * 4;
-                        p.q[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) Short4*)(from + place<D>(r, at / 8) + (at & 4) * 2));
-                    }
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c) sums[c][j] = multiply(p.v, weight[c][t], sums[c][j]);
+            for (int i = 0; i < STEPS; ++i) {
+                const int t = i / (D / 32), j = i % (D / 32);
+                if (i + 2 < STEPS) {
+                    r[(i + 2) % 3] = row_piece(slot, b, i + 2);
+                    if (kSums) c[(i + 2) % 3] = column_piece(sum_slot, sum_b, i + 2);
                 }
+                out = multiply(r[i % 3], rows[i], out);
+                if (kSums) sums[j] = multiply(c[i % 3], weight[t], sums[j]);
+                share(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
-
-        V8 weight[2][COLS][2];  // of the two blocks under way
-        Acc score[2][COLS];
+        // Units from here on hold rows that do not count: behind the last passing row, or another segment's
+        const int32_t masked = u1 == (int32_t)deal.units ? u1 - 1 : u1;
+        auto mask = [&](Acc& now, int32_t u, int b) {
+            if (u < masked) return;
+            const int64_t left = passing_rows - (int64_t)u * kSweepUnit;
+            const int32_t rows_left = u >= u1 ? 0 : left < kSweepUnit ? (int32_t)left : kSweepUnit;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c)
+            for (int r = 0; r < 16; ++r)
+                if (half * 4 >= rows_left - (b * 32 + 8 * (r / 4) + r % 4)) now[r] = -INFINITY;
+        };
+        // ---- weights of a block from its scores, 16 / STEPS' share i of them
+        constexpr int kShare = 16 / (STEPS < 16 ? STEPS : 16);
+        float part;      // the block's sum
+        uint32_t most;   // and its largest weight, as the bits of a number that is not negative
+        auto weights_of = [&](const Acc& now, V8 (&weight)[2], int i) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) weight[1][c][t] = V8{};
-
-        // Block b of unit u: its weights from its scores, while the next block's scores and the sums over the block before
-        // are made.
-        auto block = [&](int64_t u, int b) {
-            const int slot = (int)(u - u0) & (kRing - 1);
-            const int next_slot = b == 0 ? slot : (slot + 1) & (kRing - 1);
-            const int before_slot = b == 1 || u == u0 ? slot : (slot + kRing - 1) & (kRing - 1);
-            const int before_b = b == 1 ? 0 : (u == u0 ? 0 : 1);
-            Acc(&now)[COLS] = score[b];
-            if (kOnline) {
-                if (u == deal.units - 1) {  // behind the last passing row
+            for (int r = i * kShare; r < (i + 1) * kShare; ++r) {
+                float p = exp2_of(fmaf(now[r], kLog2e, -top2));
+                asm volatile("" : "+v"(p));  // made in this share
+                const uint32_t bits = __float_as_uint(p);
+                part = r == 0 ? p : part + p;
+                most = r == 0 ? bits : (most > bits ? most : bits);
+                if (kSums) weight[r / 8][r % 8] = (T)p;
+            }
+        };
+        // ---- The maximum moves only where a weight has outgrown it, and for a segment's first block: seldom.  The sums do not
+        // hold the block yet.
+        auto settle = [&](const Acc& now, V8 (&weight)[2], bool first) {
+            if (first || __ballot(most > kMost)) {
+                float t = now[0];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (u * kSweepUnit + b * 32 + 8 * (r / 4) + 4 * half + r % 4 >= passing_rows)
+                for (int r = 1; r < 16; ++r) t = fmaxf(t, now[r]);
+                t = fmaxf(top, fmaxf(t, __shfl_xor(t, 32)));
+                const float f = exp2_of((top - t) * kLog2e);
+                total *= f;
+                if (kSums)
 #pragma unroll
-                            for (int c = 0; c < COLS; ++c) now[c][r] = -INFINITY;
-                }
-                float most[COLS];
-                bool more = false;
+                    for (int j = 0; j < D / 32; ++j) sums[j] *= f;
+                top = t;
+                top2 = t * kLog2e - kRaise;
 #pragma unroll
-                for (int c = 0; c < COLS; ++c) {
-                    most[c] = now[c][0];
+                for (int i = 0; i < 16 / kShare; ++i) weights_of(now, weight, i);
+            }
+            total += part;
+        };
+        // factors of a share's rows: read a share ahead
+        typedef float Few __attribute__((ext_vector_type(kShare)));
+        Few lse_ahead, gc_ahead;
+        auto load_factors = [&](int slot, int b, int i) {
+            const int r = i * kShare;
+            const float* f = factors + slot * 3 * kSweepUnit + b * 32 + 8 * (r / 4) + half * 4 + r % 4;
+            lse_ahead = *reinterpret_cast<const Few*>(f);
+            gc_ahead = *reinterpret_cast<const Few*>(f + kSweepUnit);
+        };
+        auto dw_weights_of = [&](const Acc& now, V8 (&weight)[2], int slot, int b, int i) {
+            const Few lse = lse_ahead, gc = gc_ahead;
+            if (i + 1 < 16 / kShare) load_factors(slot, b, i + 1);
 #pragma unroll
-                    for (int r = 1; r < 16; ++r) most[c] = fmaxf(most[c], now[c][r]);
-                    more = more || most[c] > top[c] + kSlack;
-                }
-                // The maximum moves only where an exponential would outgrow it: seldom after the first blocks.
-                // Weights of the block before, not yet summed, are rounded once more then.
-                if (__ballot(more)) {
+            for (int e = 0; e < kShare; ++e) {
+                const int r = i * kShare + e;
+                float p = gc[e] * exp2_of(fmaf(now[r], kLog2e, -lse[e]));
+                asm volatile("" : "+v"(p));
+                weight[r / 8][r % 8] = (T)p;
+            }
+        };
+        // the same with the counts taken off
+        auto dw_counted = [&](const Acc& now, V8 (&weight)[2], int slot, int buffer, int b) {
+            const float* f = factors + slot * 3 * kSweepUnit + b * 32 + half * 4;
+            const char* mine = counts + buffer * Sh::kCountBytes + (wave * 32 + col) * kSweepUnit + b * 32 + half * 4;
 #pragma unroll
-                    for (int c = 0; c < COLS; ++c) {
-                        const float t = fmaxf(top[c], fmaxf(most[c], __shfl_xor(most[c], 32)));
-                        const float f = exp2_of((top[c] - t) * kLog2e);
-                        total[c] *= f;
-                        if (kSums) {
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const uint32_t c4 = *reinterpret_cast<const uint32_t*>(mine + r4 * 8);
+                const Float4 lse = *reinterpret_cast<const Float4*>(f + r4 * 8);
+                const Float4 gc = *reinterpret_cast<const Float4*>(f + kSweepUnit + r4 * 8);
+                const Float4 g = *reinterpret_cast<const Float4*>(f + 2 * kSweepUnit + r4 * 8);
 #pragma unroll
-                            for (int j = 0; j < D / 32; ++j) sums[c][j] *= f;
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) weight[b ^ 1][c][i][e] = (T)((float)weight[b ^ 1][c][i][e] * f);
-                        }
-                        top[c] = t;
-                        top2[c] = t * kLog2e - kRaise;
-                    }
-                }
-                scores(score[b ^ 1], next_slot, b ^ 1);
-                if (kSums) add_rows(weight[b ^ 1], before_slot, before_b);
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float p = exp2_of(fmaf(now[c][t * 8 + e], kLog2e, -top2[c]));
-                            total[c] += p;
-                            if (kSums) weight[b][c][t][e] = (T)p;
-                        }
-            } else {
-                const int buffer = (int)(u - u0) & 1;
-                const uint32_t held_here = wave_uniform(touched[buffer]) >> (wave * COLS * 2 + b);
-                scores(score[b ^ 1], next_slot, b ^ 1);
-                add_rows(weight[b ^ 1], before_slot, before_b);
-                const int64_t p0 = u * kSweepUnit + b * 32 + half * 4;
-#pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4) {
-                    const Float4 lse = *reinterpret_cast<const Float4*>(a.place_lse + p0 + r4 * 8);
-                    const Float4 count = *reinterpret_cast<const Float4*>(a.count + p0 + r4 * 8);
-                    const Float4 g = *reinterpret_cast<const Float4*>(a.weight + p0 + r4 * 8);
-                    const float scale = a.header->scale;
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c) {
-                        uint32_t held4 = 0;
-                        if ((held_here >> (c * 2)) & 1u)
-                            held4 = *reinterpret_cast<const uint32_t*>(counts + buffer * Sh::kCountBytes +
-                                                                       (wave * COLS * 32 + c * 32 + col) * kSweepUnit + b * 32 + r4 * 8 + half * 4);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float f = g[e] * scale;
-                            float p = f * count[e] * exp2_of((now[c][r4 * 4 + e] - lse[e]) * kLog2e);
-                            if (count[e] == 0.f) p = 0.f;
-                            p -= f * (float)((held4 >> (8 * e)) & 255u);
-                            weight[b][c][r4 / 2][r4 % 2 * 4 + e] = (T)p;
-                        }
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int r = r4 * 4 + e;
+                    const float p = gc[e] * exp2_of(fmaf(now[r], kLog2e, -lse[e]));
+                    weight[r / 8][r % 8] = (T)fmaf(-g[e], (float)((c4 >> (8 * e)) & 255u), p);
                 }
             }
         };
 
-        scores(score[0], 0, 0);
-        for (int64_t u = u0; u < u1; ++u) {
-            const int slot = (int)(u - u0) & (kRing - 1);
-            if (u + 2 < u1) {
-                keep((slot + 2) & (kRing - 1));
-                if (u + 3 < u1) load(u + 3);
+        V8 weight[2][2];  // of the two blocks under way
+        Acc score[2];
+        weight[1][0] = V8{};
+        weight[1][1] = V8{};
+        if (kAhead) scores(score[0], 0, 0);
+        // one unit; its place in LDS is known when it is compiled
+        auto step = [&](int32_t u, auto place_of) {
+            constexpr int slot = decltype(place_of)::value, buffer = slot & 1;
+            constexpr int next = (slot + 1) & (RING - 1), previous = (slot + RING - 1) & (RING - 1);
+            keep((slot + (kAhead ? 2 : 1)) & (RING - 1));
+            load(u + (kAhead ? 3 : 2));
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                // Ahead: this block's weights, while the next block's scores and the sums over the block before are made
+                // (in front of the first block: weights of zero, of a unit that starts as zeros).
+                Acc& now = score[kAhead ? b : 0];
+                V8(&mine)[2] = weight[kAhead ? b : 0];
+                const int next_slot = b == 0 ? slot : next, before_slot = b == 0 ? previous : slot;
+                if (!kAhead) scores(now, slot, b);
+                if (kOnline) {
+                    mask(now, u, b);
+                    if (kAhead)
+                        scores_and_sums(score[b ^ 1], next_slot, b ^ 1, weight[b ^ 1], before_slot, b ^ 1,
+                                        [&](int i) { weights_of(now, mine, i); });
+                    else
+#pragma unroll
+                        for (int i = 0; i < 16 / kShare; ++i) weights_of(now, mine, i);
+                    settle(now, mine, b == 0 && u == u0);
+                } else {
+                    load_factors(slot, b, 0);
+                    const bool counted = (wave_uniform(touched[buffer * 8 + wave]) >> b) & 1u;
+                    if (kAhead)
+                        scores_and_sums(score[b ^ 1], next_slot, b ^ 1, weight[b ^ 1], before_slot, b ^ 1,
+                                        [&](int i) { dw_weights_of(now, mine, slot, b, i); });
+                    else
+#pragma unroll
+                        for (int i = 0; i < 16 / kShare; ++i) dw_weights_of(now, mine, slot, b, i);
+                    if (counted) dw_counted(now, mine, slot, buffer, b);
+                }
+                if (kSums) asm volatile("" : "+v"(mine[0]), "+v"(mine[1]));  // made here, not where they are used
+                if (!kAhead && kSums) add_rows(mine, slot, b);
             }
-            block(u, 0);
-            block(u, 1);
             if (MODE == kSweepDw) {
-                const int buffer = (int)(u - u0) & 1;
+                // a wavefront clears what is counted for its rows, for the unit after the next
+                if (wave_uniform(touched[buffer * 8 + wave])) {
+                    uint4* mine = reinterpret_cast<uint4*>(counts + buffer * Sh::kCountBytes + wave * 32 * kSweepUnit);
+#pragma unroll
+                    for (int e = 0; e < 32 * kSweepUnit / 16; e += kWave) mine[e + lane] = uint4{0, 0, 0, 0};
+                    if (lane == 0) touched[buffer * 8 + wave] = 0;
+                }
                 if (u + 1 < u1) {
                     count_labels(u + 1, buffer ^ 1);
                     if (u + 2 < u1) load_labels(u + 2);
                 }
-                __syncthreads();
-                // this unit's counts are cleared for the unit after the next
-                const uint32_t dirty = wave_uniform(touched[buffer]);
-                if ((dirty >> (wave * COLS * 2)) & ((1u << (COLS * 2)) - 1u)) {
-                    uint4* mine = reinterpret_cast<uint4*>(counts + buffer * Sh::kCountBytes + wave * COLS * 32 * kSweepUnit);
-                    for (int e = lane; e < COLS * 32 * kSweepUnit / 16; e += kWave) mine[e] = uint4{0, 0, 0, 0};
-                }
-                __syncthreads();
-                if (threadIdx.x == 0) touched[buffer] = 0;
             }
-            __syncthreads();
+            lds_barrier();
+        };
+        // as many units as there is room for in LDS, whether or not all of them are the segment's: no way out in between
+        for (int32_t u = u0; u < u1; u += RING) {
+            step(u, std::integral_constant<int, 0>());
+            step(u + 1, std::integral_constant<int, 1>());
+            if constexpr (RING == 4) {
+                step(u + 2, std::integral_constant<int, 2>());
+                step(u + 3, std::integral_constant<int, 3>());
+            }
         }
-        if (kSums) add_rows(weight[1], (int)(u1 - 1 - u0) & (kRing - 1), 1);
+        if (kAhead && kSums) add_rows(weight[1], RING - 1, 1);
 
-        // out
-        const bool whole = u0 == 0 && u1 == deal.units;
+        // ---- out
         if (kOnline) {
             const int64_t segment = (int64_t)blockIdx.x + tile;
             const float lower = exp2_of(-kRaise);
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) {
-                const float both = (total[c] + __shfl_xor(total[c], 32)) * lower;
-                const int64_t at = segment * HELD + wave * (32 * COLS) + c * 32 + col;
-                if (half == 0) {
-                    s.parts.top[at] = top[c];
-                    s.parts.sum[at] = both;
-                }
-                if (kSums)
-#pragma unroll
-                    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const Float4 v = {sums[c][j][r * 4], sums[c][j][r * 4 + 1], sums[c][j][r * 4 + 2], sums[c][j][r * 4 + 3]};
-                            *reinterpret_cast<Float4*>(s.parts.rows + at * D + j * 32 + r * 8 + half * 4) = v * lower;
-                        }
+            const float both = (total + __shfl_xor(total, 32)) * lower;
+            const int64_t at = segment * HELD + wave * 32 + col;
+            if (half == 0) {
+                s.parts.top[at] = top;
+                s.parts.sum[at] = both;
             }
-        } else {
-            const float back = 1.f / a.header->scale;
-            const int64_t segment = (int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0);  // one that ends a tile, one that begins one
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) {
-                const int64_t v = row0 + c * 32 + col;
+            if (kSums)
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int e0 = j * 32 + r * 8 + half * 4;
-                        const Float4 o = {sums[c][j][r * 4], sums[c][j][r * 4 + 1], sums[c][j][r * 4 + 2], sums[c][j][r * 4 + 3]};
-                        if (!whole) {
-                            *reinterpret_cast<Float4*>(s.parts.rows + (segment * HELD + wave * (32 * COLS) + c * 32 + col) * D + e0) = o;
-                        } else if (v < held_rows) {
-                            T* to = (T*)s.out + v * s.out_stride + e0;
-                            if (e0 + 4 <= a.d) {
-                                Piece<T, 4> q;
+                        const Float4 v = {sums[j][r * 4], sums[j][r * 4 + 1], sums[j][r * 4 + 2], sums[j][r * 4 + 3]};
+                        *reinterpret_cast<Float4*>(s.parts.rows + at * D + j * 32 + r * 8 + half * 4) = v * lower;
+                    }
+        } else {
+            const bool whole = u0 == 0 && u1 == (int32_t)deal.units;
+            const float back = 1.f / scale;
+            const int64_t segment = (int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0);  // one that ends a tile, one that begins one
+            const int64_t v = row0 + col;
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) q.v[e] = (T)(o[e] * back);
-                                store_piece<T, 4>(to, q);
-                            } else {
+            for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (e0 + e < a.d) to[e] = (T)(o[e] * back);
-                            }
+                for (int r = 0; r < 4; ++r) {
+                    const int e0 = j * 32 + r * 8 + half * 4;
+                    const Float4 o = {sums[j][r * 4], sums[j][r * 4 + 1], sums[j][r * 4 + 2], sums[j][r * 4 + 3]};
+                    if (!whole) {
+                        *reinterpret_cast<Float4*>(s.parts.rows + (segment * HELD + wave * 32 + col) * D + e0) = o;
+                    } else if (v < held_rows) {
+                        T* to = (T*)s.out + v * s.out_stride + e0;
+                        if (e0 + 4 <= a.d) {
+                            Piece<T, 4> q;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) q.v[e] = (T)(o[e] * back);
+                            store_piece<T, 4>(to, q);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (e0 + e < a.d) to[e] = (T)(o[e] * back);
                         }
                     }
-            }
+                }
         }
     }
 }
@@ -399,7 +495,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kThreads
 // Rows of dw whose tile several workgroups had a part of; all of them where there was nothing to sum.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepParts parts, T* __restrict__ dw, int64_t dw_stride) {
-    constexpr int HELD = Shape<kSweepDw, D>::kHeld;
+    constexpr int HELD = kSweepHeld;
     const int64_t live = a.header->n_live;
     const SweepDeal deal(a.V, HELD, live);
     const float back = 1.f / a.header->scale;
@@ -426,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepPart
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                           int64_t w_stride, SweepParts parts, T* __restrict__ dx, int64_t dx_stride) {
-    constexpr int HELD = Shape<MODE, D>::kHeld;
+    constexpr int HELD = kSweepHeld;
     constexpr int PER = (D + 63) / 64;  // numbers of a lane: lane, lane + 64, ...
     const int64_t live = a.header->n_live;
     const SweepDeal deal(live, HELD, a.V);
@@ -513,7 +609,7 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
     if (kLds > 64 * 1024)
         ND_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&sweep_kernel<T, D, MODE>),
                                          hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
-    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(kSweepGroups), dim3(kThreads), kLds, stream, a, s);
+    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(kSweepGroups), dim3(Shape<MODE, D>::kThreads), kLds, stream, a, s);
     ND_HIP_CHECK(hipGetLastError());
     return ND_OK;
 }
@@ -521,11 +617,8 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
 }  // namespace
 
 int sweep_width(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : d <= 256 ? 256 : 0; }
-int sweep_held(int mode, int32_t dp) { return mode == kSweepLse || dp <= 128 ? 256 : 128; }
-int64_t sweep_segments(int mode, int64_t held, int32_t dp) {
-    if (mode == kSweepDw) return 2 * kSweepGroups;
-    const int h = sweep_held(mode, dp);
-    return kSweepGroups + (held + h - 1) / h;
+int64_t sweep_segments(int mode, int64_t held) {
+    return mode == kSweepDw ? 2 * kSweepGroups : kSweepGroups + (held + kSweepHeld - 1) / kSweepHeld;
 }
 
 template <typename T>
@@ -541,7 +634,6 @@ int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stri
     s.passing_stride = mode == kSweepDw ? a.dp : w_stride;
     return by_width(a.dp, [&](auto width) -> int {
         constexpr int D = decltype(width)::value;
-        static_assert(Shape<kSweepDx, D>::kHeld == Shape<kSweepDw, D>::kHeld, "sweep_held");
         if (mode == kSweepLse) return launch_sweep<T, D, kSweepLse>(a, s, stream);
         if (mode == kSweepDx) return launch_sweep<T, D, kSweepDx>(a, s, stream);
         const int rc = launch_sweep<T, D, kSweepDw>(a, s, stream);
