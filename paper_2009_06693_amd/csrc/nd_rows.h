@@ -1,0 +1,26 @@
+// Sums of rows per group, for the library's own calls.
+#pragma once
+
+#include "nd_rowtypes.h"
+
+namespace nd {
+
+constexpr int kTilePairs = 64;  // pairs of a tile (nd_rows.hip)
+
+struct GroupSum {
+    const int32_t* slots;     // n_pairs, by group
+    const int32_t* start;     // n_groups + 1
+    const int64_t* counts;    // live pairs and groups: the caller's two numbers,
+    const StepCtl* ctl;       // what the grouping left, or (both null) all
+    const int32_t* group_row; // row of the output by group (null: the group's number)
+    int64_t n_pairs, n_groups, out_rows, out_stride;
+    int32_t* tile_group;      // scratch: a group per tile of kTilePairs pairs
+    float* parts;             // scratch: [tile][first, last][d]
+};
+
+// Sums in 32-bit floats, out[u] over group u of weights[q / m] x[q / m] (weights by row).
+template <typename T>
+int group_sum_floats(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
+                     float* out, hipStream_t stream);
+
+}  // namespace nd

@@ -14,7 +14,7 @@
 #include <type_traits>
 
 #include "nd_philox.h"
-#include "nd_rowtypes.h"
+#include "nd_rows.h"
 #include "nd_wave.h"
 
 namespace nd {
@@ -206,24 +206,16 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(const T* __restri
 // Pairs are cut into tiles of equal length, whatever the groups: a hub's pairs are spread over as many workgroups as
 // they fill tiles.  A group inside one tile is summed there; of one that crosses tiles every tile leaves what it holds
 // (32-bit floats: `first` if the group began before the tile, `last` otherwise), and a second launch adds those up.
-constexpr int kTilePairs = 64;
-
-struct GroupSum {
-    const int32_t* slots;
-    const int32_t* start;
-    const int64_t* counts;
-    const int32_t* group_row;
-    int64_t n_pairs, n_groups, out_rows, out_stride;
-    int32_t* tile_group;  // group of a tile's first pair
-    float* parts;         // [tile][first, last][d]
-};
+__device__ __forceinline__ int64_t live_groups(const GroupSum& g) {
+    return g.ctl ? (int64_t)g.ctl->U : live(g.n_groups, g.counts, 1);
+}
 __device__ __forceinline__ int64_t start_of(const GroupSum& g, int64_t u, int64_t pairs) {
     const int64_t s = g.start[u];
     return s < 0 ? 0 : (s < pairs ? s : pairs);
 }
 // Live pairs that are in a group.
 __device__ __forceinline__ int64_t grouped_pairs(const GroupSum& g, int64_t groups) {
-    const int64_t pairs = live(g.n_pairs, g.counts, 0);
+    const int64_t pairs = g.ctl ? (int64_t)g.ctl->P : live(g.n_pairs, g.counts, 0);
     return groups > 0 ? start_of(g, groups, pairs) : 0;
 }
 // Row of the output that group u's sum goes to, or -1.
@@ -234,7 +226,7 @@ __device__ __forceinline__ int64_t row_of_group(const GroupSum& g, int64_t u) {
 }
 
 __global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
-    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
     const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     int64_t first = 0, last = -1;  // tiles whose first pair is this group's
     if (u < groups) {
@@ -256,16 +248,16 @@ __global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
     }
 }
 
-template <typename T, int VEC>
+template <typename T, typename O, int VEC, bool BY_ROW>
 __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict__ x, int64_t x_stride, int32_t d, Deal t,
                                                              FastDiv m, uint32_t n_slots,
                                                              const float* __restrict__ weights, GroupSum g,
-                                                             T* __restrict__ out) {
+                                                             O* __restrict__ out) {
     constexpr int kAhead = 8;
     uint32_t row;
     int32_t at;
     if (!deal_lane<VEC>(t, d, &row, &at)) return;
-    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
     for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * kTilePairs < pairs; tile += (int64_t)gridDim.x * t.rows) {
         const int64_t p0 = tile * kTilePairs;
         const int64_t p1 = p0 + kTilePairs < pairs ? p0 + kTilePairs : pairs;
@@ -285,8 +277,9 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
                 v[i] = Piece<T, VEC>{};
                 f[i] = 0.f;
                 if (q[i] < n_slots) {
-                    v[i] = load_piece<T, VEC>(x + (int64_t)fastdiv(q[i], m) * x_stride + at);
-                    f[i] = weights ? weights[q[i]] : 1.f;
+                    const uint32_t r = fastdiv(q[i], m);
+                    v[i] = load_piece<T, VEC>(x + (int64_t)r * x_stride + at);
+                    f[i] = weights ? weights[BY_ROW ? r : q[i]] : 1.f;
                 }
             }
 #pragma unroll
@@ -299,10 +292,10 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
                 if (!before && end <= p1) {
                     const int64_t r = row_of_group(g, u);
                     if (r >= 0) {
-                        Piece<T, VEC> o;
+                        Piece<O, VEC> o;
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
-                        store_piece<T, VEC>(out + r * g.out_stride + at, o);
+                        for (int e = 0; e < VEC; ++e) o.v[e] = (O)sum[e];
+                        store_piece<O, VEC>(out + r * g.out_stride + at, o);
                     }
                 } else {
                     Piece<float, VEC> o;
@@ -329,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
     uint32_t row;
     int32_t at;
     const bool mine = deal_lane<VEC>(t, d, &row, &at);
-    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
     // a workgroup looks through 64 groups at a time and joins those that cross tiles; groups without pairs are zero rows
     for (int64_t u0 = (int64_t)blockIdx.x * kWave; u0 < groups; u0 += (int64_t)gridDim.x * kWave) {
         int64_t a = 0, b = 1;
@@ -375,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
 template <typename T, int VEC>
 __global__ __launch_bounds__(kThreads) void group_clear_kernel(int32_t d, GroupSum g, T* __restrict__ out) {
     __shared__ uint32_t named[kThreads];
-    const int64_t groups = live(g.n_groups, g.counts, 1), pairs = grouped_pairs(g, groups);
+    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
     const int64_t r0 = (int64_t)blockIdx.x * kThreads;
     const int64_t r1 = r0 + kThreads < g.out_rows ? r0 + kThreads : g.out_rows;
     int64_t lo = 0, hi = groups;  // first group with a row of r0 or more
@@ -407,6 +400,25 @@ __global__ __launch_bounds__(kThreads) void group_clear_kernel(int32_t d, GroupS
 }
 
 // ------------------------------------------------------------------------------------------------------ launches
+template <typename T, typename O, int VEC, bool BY_ROW>
+int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
+                     O* out, hipStream_t stream) {
+    const Deal t = make_deal(d, VEC);
+    const int64_t tiles = (g.n_pairs + kTilePairs - 1) / kTilePairs;
+    if (g.n_groups > 0 && tiles > 0) {
+        hipLaunchKernelGGL(group_tiles_kernel, dim3((unsigned)((g.n_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                           stream, g);
+        hipLaunchKernelGGL((group_sum_kernel<T, O, VEC, BY_ROW>), dim3(workgroups((tiles + t.rows - 1) / t.rows), deal_columns(t)),
+                           dim3(deal_threads(t)), 0, stream, x, x_stride, d, t, make_fastdiv((uint32_t)m), (uint32_t)(n * m),
+                           weights, g, out);
+    }
+    if (g.n_groups > 0)
+        hipLaunchKernelGGL((group_join_kernel<O, VEC>), dim3(workgroups((g.n_groups + kWave - 1) / kWave), deal_columns(t)),
+                           dim3(deal_threads(t)), 0, stream, d, t, g, out);
+    ND_HIP_CHECK(hipGetLastError());
+    return ND_OK;
+}
+
 template <typename F>
 int by_type(int dtype, F&& f) {
     switch (dtype) {
@@ -448,6 +460,18 @@ GroupSumPlan plan_group_sum(int64_t n_pairs, int32_t d) {
 }
 
 }  // namespace
+
+// Rows of whole pieces only.
+template <typename T>
+int group_sum_floats(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
+                     float* out, hipStream_t stream) {
+    return launch_group_sum<T, float, 16 / (int)sizeof(T), true>(x, x_stride, n, d, m, weights, g, out, stream);
+}
+template int group_sum_floats<bf16_t>(const bf16_t*, int64_t, int64_t, int32_t, int32_t, const float*, const GroupSum&, float*,
+                                      hipStream_t);
+template int group_sum_floats<f16_t>(const f16_t*, int64_t, int64_t, int32_t, int32_t, const float*, const GroupSum&, float*,
+                                     hipStream_t);
+
 }  // namespace nd
 
 using namespace nd;
@@ -622,22 +646,12 @@ int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n,
         using T = std::remove_pointer_t<decltype(type)>;
         return by_width<T>(d, [&](auto width) -> int {
             constexpr int VEC = decltype(width)::value;
-            const Deal t = make_deal(d, VEC);
-            if (group_row_dev)
+            if (group_row_dev) {
                 hipLaunchKernelGGL((group_clear_kernel<T, VEC>), dim3((unsigned)((out_rows + kThreads - 1) / kThreads)),
                                    dim3(kThreads), 0, stream, d, g, (T*)out_dev);
-            if (n_groups > 0 && n_pairs > 0) {
-                hipLaunchKernelGGL(group_tiles_kernel, dim3((unsigned)((n_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                                   stream, g);
-                hipLaunchKernelGGL((group_sum_kernel<T, VEC>), dim3(workgroups((plan.tiles + t.rows - 1) / t.rows), deal_columns(t)),
-                                   dim3(deal_threads(t)), 0, stream, (const T*)x_dev, x_stride, d, t, make_fastdiv((uint32_t)m),
-                                   (uint32_t)(n * m), weights_dev, g, (T*)out_dev);
+                ND_HIP_CHECK(hipGetLastError());
             }
-            if (n_groups > 0)
-                hipLaunchKernelGGL((group_join_kernel<T, VEC>), dim3(workgroups((n_groups + kWave - 1) / kWave), deal_columns(t)),
-                                   dim3(deal_threads(t)), 0, stream, d, t, g, (T*)out_dev);
-            ND_HIP_CHECK(hipGetLastError());
-            return ND_OK;
+            return launch_group_sum<T, T, VEC, false>((const T*)x_dev, x_stride, n, d, m, weights_dev, g, (T*)out_dev, stream);
         });
     });
 }

@@ -10,6 +10,7 @@
 #include <cfloat>
 #include <type_traits>
 
+#include "nd_rows.h"
 #include "nd_sweep.h"
 #include "nd_wave.h"
 
@@ -127,6 +128,9 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* _
         } else if (row < a.n) {
             a.loss[row] = 0.f;
             a.lse[row] = 0.f;
+            // the places behind the last row that counts have no labels; this row's share of them
+            const int64_t p = all + (row - (before + at));
+            for (int32_t j = 0; j < a.k; ++j) a.labels_of[p * a.k + j] = -1;
         }
     }
     __syncthreads();
@@ -166,6 +170,17 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(const T* __restrict__ w, 
         for (int32_t e = lane_id(); e < dp; e += kWave) out[r * dp + e] = e < d ? w[r * stride + e] : (T)0.f;
 }
 
+// Which row of the sums over labels is a vertex's: none, then those of the groups.
+__global__ __launch_bounds__(kThreads) void label_clear_kernel(int32_t* __restrict__ label_row, int64_t V) {
+    const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (v < V) label_row[v] = -1;
+}
+__global__ __launch_bounds__(kThreads) void label_rows_kernel(const StepCtl* __restrict__ ctl, const int32_t* __restrict__ key,
+                                                              int64_t most, int32_t* __restrict__ label_row) {
+    const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (u < most && u < (int64_t)ctl->U) label_row[key[u]] = (int32_t)u;
+}
+
 // ------------------------------------------------------------------------------------------------ product of tiles
 // C[m][n] = sum_k A(m, k) B(n, k) for a tile of 128 x 128, four wavefronts of 64 x 64 each in 32 x 32 matrix
 // instructions.  An operand lies in memory with the summed dimension along its rows (ACROSS = false) or down its columns
@@ -194,8 +209,9 @@ __device__ __forceinline__ int lds_place(int r, int c) {
     return (r * 16 + (c ^ (((r & 3) << 2) | ((r >> 2) & 3)))) * kChunk;                        // 64 rows of 16 pieces
 }
 
+typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
 struct Chunks {
-    uint4 v[4];
+    Word4 v[4];
 };
 template <typename T, bool ACROSS>
 __device__ __forceinline__ void fetch(const Operand<T>& o, int64_t m0, int64_t k0, Chunks& c) {
@@ -207,7 +223,7 @@ __device__ __forceinline__ void fetch(const Operand<T>& o, int64_t m0, int64_t k
         row = row < o.rows ? row : o.rows - 1;
         int64_t col = (ACROSS ? m0 : k0) + p * Kind<T>::kVec;
         if (ACROSS && col > o.cols - Kind<T>::kVec) col = o.cols - Kind<T>::kVec;
-        c.v[i] = *reinterpret_cast<const uint4*>(o.base + row * o.stride + col);
+        c.v[i] = *reinterpret_cast<const Word4*>(o.base + row * o.stride + col);
     }
 }
 template <typename T, bool ACROSS>
@@ -216,7 +232,7 @@ __device__ __forceinline__ void keep(char* lds, const Chunks& c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int e = i * kThreads + (int)threadIdx.x;
-        *reinterpret_cast<uint4*>(lds + lds_place<T, ACROSS>(e / kPieces, e % kPieces)) = c.v[i];
+        *reinterpret_cast<Word4*>(lds + lds_place<T, ACROSS>(e / kPieces, e % kPieces)) = c.v[i];
     }
 }
 
@@ -528,6 +544,10 @@ struct LossPlan {
     int64_t n_pad, blocks, piece;   // piece: vertices at a time (a multiple of a tile)
     int32_t dp, groups, shares;
     bool sweep;                     // rows short enough for nd_sweep.hip
+    // labels by vertex: the grouping's arrays, sums of their rows
+    int64_t label_groups;
+    SortPlan sort;
+    size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group, o_label_parts;
     size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, total;
 };
 LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool grad) {
@@ -578,6 +598,25 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
         p.o_max = take(held * 4);
         p.o_sum = take(held * 4);
         p.o_parts = take(sums * (size_t)p.dp * 4);
+        if (grad) {
+            const size_t slots = (size_t)n * (size_t)k, some = slots > 0 ? slots : 1;
+            const size_t tiles = (slots + kTilePairs - 1) / kTilePairs;
+            p.label_groups = (int64_t)slots < V ? (int64_t)slots : V;
+            p.sort = make_sort_plan((int64_t)slots, V);
+            p.o_ctl = take(sizeof(StepCtl));
+            for (int i = 0; i < 2; ++i) {
+                p.o_keys[i] = take(some * 4);
+                p.o_vals[i] = take(some * 4);
+            }
+            p.o_hist = take(sort_hist_bytes(p.sort));
+            p.o_scratch = take(seg_scratch_bytes((int64_t)slots));
+            p.o_gkey = take(some * 4);
+            p.o_gstart = take((some + 1) * 4);
+            p.o_label_row = take((size_t)V * 4);
+            p.o_label_sums = take((size_t)p.label_groups * (size_t)p.dp * 4);
+            p.o_tile_group = take(tiles * 4);
+            p.o_label_parts = take(tiles * 2 * (size_t)p.dp * 4);
+        }
         p.total = o;
         return p;
     }
@@ -619,6 +658,36 @@ struct LossCall {
     bool grad;
 };
 
+// The rows under every vertex that is a label, summed: the part of dw that labels have.
+template <typename T>
+int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, SweepParts* parts, hipStream_t stream) {
+    const int64_t slots = a.n * a.k;
+    StepCtl* ctl = (StepCtl*)(ws + p.o_ctl);
+    int32_t *keys = nullptr, *vals = nullptr, *g_key = (int32_t*)(ws + p.o_gkey), *g_start = (int32_t*)(ws + p.o_gstart);
+    int32_t* label_row = (int32_t*)(ws + p.o_label_row);
+    int rc = sort_pairs(a.labels_of, slots, (int32_t)a.V, p.sort, (int32_t*)(ws + p.o_keys[0]), (int32_t*)(ws + p.o_vals[0]),
+                        (int32_t*)(ws + p.o_keys[1]), (int32_t*)(ws + p.o_vals[1]), (uint32_t*)(ws + p.o_hist), ctl, nullptr,
+                        1, nullptr, &keys, &vals, stream);
+    if (rc == ND_OK) rc = build_groups(keys, slots, ctl, g_key, g_start, (uint32_t*)(ws + p.o_scratch), nullptr, 0, stream);
+    if (rc != ND_OK) return rc;
+    hipLaunchKernelGGL(label_clear_kernel, dim3((unsigned)((a.V + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, label_row, a.V);
+    hipLaunchKernelGGL(label_rows_kernel, dim3((unsigned)((p.label_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, ctl,
+                       g_key, p.label_groups, label_row);
+    ND_HIP_CHECK(hipGetLastError());
+    GroupSum g{};
+    g.slots = vals;
+    g.start = g_start;
+    g.ctl = ctl;
+    g.n_pairs = slots;
+    g.n_groups = g.out_rows = p.label_groups;
+    g.out_stride = a.dp;
+    g.tile_group = (int32_t*)(ws + p.o_tile_group);
+    g.parts = (float*)(ws + p.o_label_parts);
+    parts->label_row = label_row;
+    parts->label_sums = (const float*)(ws + p.o_label_sums);
+    return group_sum_floats<T>(rows, a.dp, p.n_pad, a.dp, a.k, a.weight, g, (float*)(ws + p.o_label_sums), stream);
+}
+
 template <typename T>
 int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream) {
     LossArgs a{};
@@ -652,7 +721,8 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
                        c.grad ? (T*)c.dx : nullptr, c.dx_stride, (int32_t)blocks);
     const T* w = (const T*)c.w;
     int64_t w_stride = c.w_stride;
-    const bool as_it_is = c.d == p.dp && w_stride * (int64_t)sizeof(T) % kChunk == 0 && (uintptr_t)w % kChunk == 0;
+    // a stride beyond 2^24 numbers would leave 32 bits within a sweep's unit
+    const bool as_it_is = c.d == p.dp && w_stride < (1 << 24) && w_stride * (int64_t)sizeof(T) % kChunk == 0 && (uintptr_t)w % kChunk == 0;
     if (!as_it_is) {
         T* padded = (T*)(ws + p.o_w);
         const int64_t quads = (c.V + 3) / 4;
@@ -663,13 +733,14 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     }
     if constexpr (sizeof(T) == 2)
         if (p.sweep) {
-            const SweepParts parts{a.part_max, a.part_sum, (float*)(ws + p.o_parts)};
+            SweepParts parts{a.part_max, a.part_sum, (float*)(ws + p.o_parts), nullptr, nullptr};
             const int mode = c.grad && c.dx ? kSweepDx : kSweepLse;
             int rc = ND_OK;
             if (c.n > 0) {
                 rc = sweep<T>(mode, a, rows, w, w_stride, parts, nullptr, 0, stream);
                 if (rc == ND_OK) rc = sweep_finish<T>(mode, a, rows, w, w_stride, parts, (T*)c.dx, c.dx_stride, stream);
             }
+            if (rc == ND_OK && c.grad && c.dw && c.n > 0) rc = sum_labels<T>(a, p, ws, rows, &parts, stream);
             if (rc == ND_OK && c.grad && c.dw) rc = sweep<T>(kSweepDw, a, rows, w, w_stride, parts, (T*)c.dw, c.dw_stride, stream);
             return rc;
         }

@@ -14,7 +14,7 @@ constexpr int kSweepLeast = 4;      // units that a workgroup takes at least
 enum SweepMode {
     kSweepLse = 0,   // x held, w passes: maximum and sum of exponentials per row of x
     kSweepDx = 1,    // the same, and the sums of w's rows weighted with the exponentials
-    kSweepDw = 2,    // w held, x passes: sums of x's rows weighted with g (c p - count)
+    kSweepDw = 2,    // w held, x passes: sums of x's rows weighted with g c p, less the sums over labels
 };
 
 // How the work, tiles of held rows x units of passing rows, is dealt out: workgroup g takes the units
@@ -74,6 +74,9 @@ struct LossArgs {
 struct SweepParts {
     float *top, *sum;   // [segment][held rows of a tile]
     float* rows;        // [segment][held rows of a tile][dp]
+    // kSweepDw: by vertex, the row of label_sums with the sum of its labels' rows, or -1
+    const int32_t* label_row;
+    const float* label_sums;
 };
 int sweep_width(int32_t d);                   // numbers in a padded row, 0: rows are too long
 int64_t sweep_segments(int mode, int64_t held);

@@ -3,7 +3,6 @@
 #include <cfloat>
 #include <type_traits>
 
-#include "nd_philox.h"
 #include "nd_wave.h"
 
 // With h a tile of held rows and p a block of 32 passing rows, a wavefront makes
@@ -23,6 +22,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef short Short4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 struct Eight {
@@ -48,10 +48,8 @@ struct Shape {
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
     static constexpr int kUnitBytes = kSweepUnit * D * 2;
     static constexpr int kLoads = kUnitBytes / (kThreads * 16);  // pieces that a lane moves per unit
-    // kSweepDw: what the passing rows weigh, and counts of labels, a byte per (held row, passing row) of a unit, two units
-    static constexpr int kFactorBytes = MODE == kSweepDw ? 3 * kSweepUnit * 4 : 0;
-    static constexpr int kCountBytes = MODE == kSweepDw ? kHeld * kSweepUnit : 0;
-    static constexpr int kLds = kRing * (kUnitBytes + kFactorBytes) + 2 * kCountBytes + (MODE == kSweepDw ? 64 : 0);
+    static constexpr int kFactorBytes = MODE == kSweepDw ? 2 * kSweepUnit * 4 : 0;  // what the passing rows weigh
+    static constexpr int kLds = kRing * (kUnitBytes + kFactorBytes);
 };
 
 // Byte position of piece c of row r of a unit: pieces change places so that 16 rows' reads of one piece, and 4 rows' reads of
@@ -98,17 +96,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
     if ((int64_t)blockIdx.x >= deal.groups) return;
     const T* held = (const T*)s.held;
     const T* passing = (const T*)s.passing;
-    float* factors = (float*)(lds + RING * Sh::kUnitBytes);                    // [unit][lse log2 e, g c, g][passing row]
-    char* counts = lds + RING * (Sh::kUnitBytes + Sh::kFactorBytes);           // [unit][held row][passing row]
-    uint32_t* touched = (uint32_t*)(counts + 2 * Sh::kCountBytes);             // [unit][wavefront]: a bit per block with counts
+    float* factors = (float*)(lds + RING * Sh::kUnitBytes);                    // [unit][lse log2 e, g c][passing row]
     const float scale = MODE == kSweepDw ? a.header->scale : 1.f;
 
-    uint32_t load_at[Sh::kLoads];  // where a lane's pieces of a unit lie
-#pragma unroll
-    for (int i = 0; i < Sh::kLoads; ++i) {
-        const int e = i * THREADS + (int)threadIdx.x;
-        load_at[i] = (uint32_t)(e / Sh::kPieces) * (uint32_t)s.passing_stride + e % Sh::kPieces * 8;
-    }
     // where a lane reads in a unit: pieces of a row (a block's 32 rows), and four rows of a column's 8 bytes (16 rows); what
     // the kernel adds to them is known when it is compiled
     typedef LdsOf<char> LdsChar;
@@ -124,6 +114,10 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
             column_at[e][j] = place<D>(e * 8 + half * 4 + (sub >> 2), at / 8) + (at & 4) * 2;
         }
 
+    // behind what an instruction's offset reaches from the front of LDS: the lane's own place, kept in a register
+    LdsChar* factor_lds = unit_lds + RING * Sh::kUnitBytes + half * 16;
+    if (MODE == kSweepDw) asm volatile("" : "+v"(factor_lds));
+
     const int64_t end = deal.first((int64_t)blockIdx.x + 1);
     for (int64_t x = deal.first(blockIdx.x); x < end;) {
         const int64_t tile = x / deal.units;
@@ -133,71 +127,41 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         x += u1 - u0;
 
         // ---- passing rows on their way to LDS
-        uint4 ahead[Sh::kLoads];
+        Word4 ahead[Sh::kLoads];
         float factor_ahead[3];
         auto load = [&](int32_t u) {
             // gathered rows are padded with zeros to whole units, but no further
-            const int64_t r0 = (int64_t)u * kSweepUnit, last = (MODE == kSweepDw ? deal.units * kSweepUnit : passing_rows) - 1 - r0;
-            const T* from = passing + r0 * s.passing_stride;
-            if (last >= kSweepUnit - 1) {
+            // No branches: what is loaded must not be waited for here.  Rows behind the last one are the last one again;
+            // gathered rows are padded with zeros to whole units, but no further.
+            const int64_t r0 = (int64_t)u * kSweepUnit, left = (MODE == kSweepDw ? deal.units * kSweepUnit : passing_rows) - r0;
+            const int64_t from_row = left > 0 ? r0 : 0;
+            const uint32_t last = left > kSweepUnit ? kSweepUnit - 1 : left > 0 ? (uint32_t)left - 1u : 0u;
+            const char* from = (const char*)(passing + from_row * s.passing_stride);
+            const uint32_t row_bytes = (uint32_t)s.passing_stride * 2u;
 #pragma unroll
-                for (int i = 0; i < Sh::kLoads; ++i) ahead[i] = *reinterpret_cast<const uint4*>(from + load_at[i]);
-            } else {  // rows behind the last one are the last one again
-#pragma unroll
-                for (int i = 0; i < Sh::kLoads; ++i) {
-                    const int e = i * THREADS + (int)threadIdx.x;
-                    const int64_t r = e / Sh::kPieces < last ? e / Sh::kPieces : last;
-                    ahead[i] = *reinterpret_cast<const uint4*>(from + r * s.passing_stride + e % Sh::kPieces * 8);
-                }
+            for (int i = 0; i < Sh::kLoads; ++i) {
+                const uint32_t e = (uint32_t)(i * THREADS) + threadIdx.x, r = e / Sh::kPieces;
+                ahead[i] = *reinterpret_cast<const Word4*>(from + ((r < last ? r : last) * row_bytes + e % Sh::kPieces * 16u));
             }
-            if (MODE == kSweepDw && threadIdx.x < kSweepUnit) {
-                factor_ahead[0] = INFINITY;  // behind the segment's last unit nothing weighs
-                factor_ahead[1] = 0.f;
-                factor_ahead[2] = 0.f;
-                if (u < u1) {
-                    const int64_t p = r0 + threadIdx.x;
-                    const float g = a.weight[p] * scale;
-                    factor_ahead[0] = a.place_lse[p] * kLog2e;
-                    factor_ahead[1] = g * a.count[p];
-                    factor_ahead[2] = g;
-                }
+            if (MODE == kSweepDw) {
+                const int64_t p = from_row + (threadIdx.x & (kSweepUnit - 1));
+                factor_ahead[0] = a.place_lse[p];
+                factor_ahead[1] = a.count[p];
+                factor_ahead[2] = a.weight[p];
             }
         };
-        auto keep = [&](int slot) {
+        auto keep = [&](int32_t u, int slot) {
 #pragma unroll
             for (int i = 0; i < Sh::kLoads; ++i) {
                 const int e = i * THREADS + (int)threadIdx.x;
-                *reinterpret_cast<uint4*>(lds + slot * Sh::kUnitBytes + place<D>(e / Sh::kPieces, e % Sh::kPieces)) = ahead[i];
+                *reinterpret_cast<Word4*>(lds + slot * Sh::kUnitBytes + place<D>(e / Sh::kPieces, e % Sh::kPieces)) = ahead[i];
             }
-            if (MODE == kSweepDw && threadIdx.x < kSweepUnit)
-#pragma unroll
-                for (int i = 0; i < 3; ++i) factors[(slot * 3 + i) * kSweepUnit + threadIdx.x] = factor_ahead[i];
-        };
-
-        // ---- labels of a unit's rows that are among the held ones
-        constexpr int kLabelLoads = MODE == kSweepDw ? 2 : 1;
-        const uint32_t unit_labels = (uint32_t)(kSweepUnit * a.k);
-        int32_t met[kLabelLoads];
-        auto load_labels = [&](int32_t u) {
-#pragma unroll
-            for (int i = 0; i < kLabelLoads; ++i) {
-                const uint32_t e = (uint32_t)(i * THREADS) + threadIdx.x;
-                met[i] = e < unit_labels ? a.labels_of[(int64_t)u * unit_labels + e] : -1;
+            if (MODE == kSweepDw && threadIdx.x < kSweepUnit) {
+                // behind the segment's last unit nothing weighs
+                float* f = factors + slot * 2 * kSweepUnit + threadIdx.x;
+                f[0] = u < u1 ? factor_ahead[0] * kLog2e : INFINITY;
+                f[kSweepUnit] = u < u1 ? factor_ahead[1] * factor_ahead[2] * scale : 0.f;
             }
-        };
-        const int64_t held0 = tile * HELD;
-        auto count_label = [&](int32_t v, uint32_t e, int buffer) {
-            const uint64_t h = (uint64_t)((int64_t)v - held0);
-            if (v < 0 || h >= (uint64_t)HELD) return;
-            const uint32_t r = fastdiv(e, a.div_k), at = (uint32_t)h * kSweepUnit + r;
-            atomicAdd((uint32_t*)(counts + buffer * Sh::kCountBytes + (at & ~3u)), 1u << (8u * (at & 3u)));
-            atomicOr(&touched[buffer * 8 + h / 32u], 1u << (r / 32u));
-        };
-        auto count_labels = [&](int32_t u, int buffer) {
-#pragma unroll
-            for (int i = 0; i < kLabelLoads; ++i) count_label(met[i], (uint32_t)(i * THREADS) + threadIdx.x, buffer);
-            for (uint32_t e = (uint32_t)(kLabelLoads * THREADS) + threadIdx.x; e < unit_labels; e += THREADS)
-                count_label(a.labels_of[(int64_t)u * unit_labels + e], e, buffer);
         };
 
         // ---- held rows, as operands
@@ -215,28 +179,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         float top = -FLT_MAX, top2 = 0.f, total = 0.f;  // maximum, the same in the exponent of 2, sum
 
         lds_barrier();  // the segment before has read its units
-        if (MODE == kSweepDw) {
-            for (int e = threadIdx.x * 16; e < 2 * Sh::kCountBytes; e += THREADS * 16)
-                *reinterpret_cast<uint4*>(counts + e) = uint4{0, 0, 0, 0};
-            if (threadIdx.x < 16) touched[threadIdx.x] = 0;
-            load_labels(u0);
-        }
         if (kAhead)  // what the sums read in front of the first block
             for (int e = threadIdx.x * 16; e < Sh::kUnitBytes; e += THREADS * 16)
-                *reinterpret_cast<uint4*>(lds + (RING - 1) * Sh::kUnitBytes + e) = uint4{0, 0, 0, 0};
+                *reinterpret_cast<Word4*>(lds + (RING - 1) * Sh::kUnitBytes + e) = Word4{0, 0, 0, 0};
         load(u0);
-        keep(0);
+        keep(u0, 0);
         if (kAhead) {
             load(u0 + 1);
-            keep(1);
+            keep(u0 + 1, 1);
         }
         load(u0 + (kAhead ? 2 : 1));
         lds_barrier();
-        if (MODE == kSweepDw) {
-            count_labels(u0, 0);
-            if (u0 + 1 < u1) load_labels(u0 + 1);
-            lds_barrier();
-        }
 
         // ---- operands from LDS: a piece of 32 passing rows for the scores; 16 passing rows down 32 columns for the sums
         auto row_piece = [&](int slot, int b, int k) {
@@ -341,9 +294,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         Few lse_ahead, gc_ahead;
         auto load_factors = [&](int slot, int b, int i) {
             const int r = i * kShare;
-            const float* f = factors + slot * 3 * kSweepUnit + b * 32 + 8 * (r / 4) + half * 4 + r % 4;
-            lse_ahead = *reinterpret_cast<const Few*>(f);
-            gc_ahead = *reinterpret_cast<const Few*>(f + kSweepUnit);
+            const int at = (slot * 2 * kSweepUnit + b * 32 + 8 * (r / 4) + r % 4) * 4;
+            lse_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at);
+            gc_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at + kSweepUnit * 4);
         };
         auto dw_weights_of = [&](const Acc& now, V8 (&weight)[2], int slot, int b, int i) {
             const Few lse = lse_ahead, gc = gc_ahead;
@@ -356,24 +309,6 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                 weight[r / 8][r % 8] = (T)p;
             }
         };
-        // the same with the counts taken off
-        auto dw_counted = [&](const Acc& now, V8 (&weight)[2], int slot, int buffer, int b) {
-            const float* f = factors + slot * 3 * kSweepUnit + b * 32 + half * 4;
-            const char* mine = counts + buffer * Sh::kCountBytes + (wave * 32 + col) * kSweepUnit + b * 32 + half * 4;
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const uint32_t c4 = *reinterpret_cast<const uint32_t*>(mine + r4 * 8);
-                const Float4 lse = *reinterpret_cast<const Float4*>(f + r4 * 8);
-                const Float4 gc = *reinterpret_cast<const Float4*>(f + kSweepUnit + r4 * 8);
-                const Float4 g = *reinterpret_cast<const Float4*>(f + 2 * kSweepUnit + r4 * 8);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = r4 * 4 + e;
-                    const float p = gc[e] * exp2_of(fmaf(now[r], kLog2e, -lse[e]));
-                    weight[r / 8][r % 8] = (T)fmaf(-g[e], (float)((c4 >> (8 * e)) & 255u), p);
-                }
-            }
-        };
 
         V8 weight[2][2];  // of the two blocks under way
         Acc score[2];
@@ -382,9 +317,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         if (kAhead) scores(score[0], 0, 0);
         // one unit; its place in LDS is known when it is compiled
         auto step = [&](int32_t u, auto place_of) {
-            constexpr int slot = decltype(place_of)::value, buffer = slot & 1;
+            constexpr int slot = decltype(place_of)::value;
             constexpr int next = (slot + 1) & (RING - 1), previous = (slot + RING - 1) & (RING - 1);
-            keep((slot + (kAhead ? 2 : 1)) & (RING - 1));
+            keep(u + (kAhead ? 2 : 1), (slot + (kAhead ? 2 : 1)) & (RING - 1));
             load(u + (kAhead ? 3 : 2));
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -405,30 +340,15 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                     settle(now, mine, b == 0 && u == u0);
                 } else {
                     load_factors(slot, b, 0);
-                    const bool counted = (wave_uniform(touched[buffer * 8 + wave]) >> b) & 1u;
                     if (kAhead)
                         scores_and_sums(score[b ^ 1], next_slot, b ^ 1, weight[b ^ 1], before_slot, b ^ 1,
                                         [&](int i) { dw_weights_of(now, mine, slot, b, i); });
                     else
 #pragma unroll
                         for (int i = 0; i < 16 / kShare; ++i) dw_weights_of(now, mine, slot, b, i);
-                    if (counted) dw_counted(now, mine, slot, buffer, b);
                 }
                 if (kSums) asm volatile("" : "+v"(mine[0]), "+v"(mine[1]));  // made here, not where they are used
                 if (!kAhead && kSums) add_rows(mine, slot, b);
-            }
-            if (MODE == kSweepDw) {
-                // a wavefront clears what is counted for its rows, for the unit after the next
-                if (wave_uniform(touched[buffer * 8 + wave])) {
-                    uint4* mine = reinterpret_cast<uint4*>(counts + buffer * Sh::kCountBytes + wave * 32 * kSweepUnit);
-#pragma unroll
-                    for (int e = 0; e < 32 * kSweepUnit / 16; e += kWave) mine[e + lane] = uint4{0, 0, 0, 0};
-                    if (lane == 0) touched[buffer * 8 + wave] = 0;
-                }
-                if (u + 1 < u1) {
-                    count_labels(u + 1, buffer ^ 1);
-                    if (u + 2 < u1) load_labels(u + 2);
-                }
             }
             lds_barrier();
         };
@@ -466,6 +386,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
             const float back = 1.f / scale;
             const int64_t segment = (int64_t)blockIdx.x * 2 + (u0 == 0 ? 1 : 0);  // one that ends a tile, one that begins one
             const int64_t v = row0 + col;
+            const int32_t labels = whole && v < held_rows ? s.parts.label_row[v] : -1;
+            const float* label_sum = s.parts.label_sums + (int64_t)labels * D;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
@@ -475,16 +397,18 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                     if (!whole) {
                         *reinterpret_cast<Float4*>(s.parts.rows + (segment * HELD + wave * 32 + col) * D + e0) = o;
                     } else if (v < held_rows) {
+                        Float4 less = {};
+                        if (labels >= 0) less = *reinterpret_cast<const Float4*>(label_sum + e0);
                         T* to = (T*)s.out + v * s.out_stride + e0;
-                        if (e0 + 4 <= a.d) {
-                            Piece<T, 4> q;
+                        Piece<T, 4> q;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) q.v[e] = (T)(o[e] * back);
+                        for (int e = 0; e < 4; ++e) q.v[e] = (T)fmaf(o[e], back, -less[e]);
+                        if (e0 + 4 <= a.d) {
                             store_piece<T, 4>(to, q);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (e0 + e < a.d) to[e] = (T)(o[e] * back);
+                                if (e0 + e < a.d) to[e] = q.v[e];
                         }
                     }
                 }
@@ -507,13 +431,14 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepPart
             g1 = deal.group_of(x0 + deal.units - 1);
             if (g0 == g1) continue;
         }
+        const int32_t labels = live > 0 ? parts.label_row[v] : -1;
         for (int e = lane_id(); e < a.d; e += kWave) {
             float sum = 0.f;
             for (int64_t g = g0; g <= g1; ++g) {
                 const int64_t segment = g * 2 + (deal.first(g) <= x0 ? 1 : 0);
                 sum += parts.rows[(segment * HELD + v % HELD) * D + e];
             }
-            dw[v * dw_stride + e] = (T)(sum * back);
+            dw[v * dw_stride + e] = (T)(sum * back - (labels >= 0 ? parts.label_sums[(int64_t)labels * D + e] : 0.f));
         }
     }
 }
