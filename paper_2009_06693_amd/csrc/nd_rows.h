@@ -5,7 +5,7 @@
 
 namespace nd {
 
-constexpr int kTilePairs = 64;  // pairs of a tile (nd_rows.hip)
+int64_t group_sum_tiles(int64_t n_pairs, int32_t d, int dtype);  // what the scratch arrays are sized by
 
 struct GroupSum {
     const int32_t* slots;     // n_pairs, by group
@@ -14,8 +14,9 @@ struct GroupSum {
     const StepCtl* ctl;       // what the grouping left, or (both null) all
     const int32_t* group_row; // row of the output by group (null: the group's number)
     int64_t n_pairs, n_groups, out_rows, out_stride;
-    int32_t* tile_group;      // scratch: a group per tile of kTilePairs pairs
+    int32_t* tile_group;      // scratch: a group per tile of pairs
     float* parts;             // scratch: [tile][first, last][d]
+    int32_t tile;             // pairs of a tile (filled in)
 };
 
 // Sums in 32-bit floats, out[u] over group u of weights[q / m] x[q / m] (weights by row).

@@ -232,8 +232,8 @@ __global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
     if (u < groups) {
         const int64_t a = start_of(g, u, pairs), b = start_of(g, u + 1, pairs);
         if (b > a) {
-            first = (a + kTilePairs - 1) / kTilePairs;
-            last = (b - 1) / kTilePairs;
+            first = (a + g.tile - 1) / g.tile;
+            last = (b - 1) / g.tile;
         }
     }
     // few: every lane its own; many (a hub): the wavefront together
@@ -258,9 +258,9 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
     int32_t at;
     if (!deal_lane<VEC>(t, d, &row, &at)) return;
     const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
-    for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * kTilePairs < pairs; tile += (int64_t)gridDim.x * t.rows) {
-        const int64_t p0 = tile * kTilePairs;
-        const int64_t p1 = p0 + kTilePairs < pairs ? p0 + kTilePairs : pairs;
+    for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * g.tile < pairs; tile += (int64_t)gridDim.x * t.rows) {
+        const int64_t p0 = tile * g.tile;
+        const int64_t p1 = p0 + g.tile < pairs ? p0 + g.tile : pairs;
         int64_t u = (uint32_t)g.tile_group[tile];
         if (u >= groups) u = groups - 1;
         bool before = start_of(g, u, pairs) < p0;
@@ -315,7 +315,17 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
     }
 }
 
-// Adds up what tiles left of a group, a workgroup's rows of lanes taking every rows-th tile of a group.
+template <typename T, int VEC>
+__device__ __forceinline__ void store_group(const GroupSum& g, int64_t u, int32_t at, const float (&sum)[VEC], T* __restrict__ out) {
+    const int64_t r = row_of_group(g, u);
+    if (r < 0) return;
+    Piece<T, VEC> o;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
+    store_piece<T, VEC>(out + r * g.out_stride + at, o);
+}
+
+// Adds up what tiles left of a group.
 template <typename T, int VEC>
 __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t, GroupSum g, T* __restrict__ out) {
     __shared__ float shared[kThreads * VEC];
@@ -323,24 +333,39 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
     int32_t at;
     const bool mine = deal_lane<VEC>(t, d, &row, &at);
     const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
-    // a workgroup looks through 64 groups at a time and joins those that cross tiles; groups without pairs are zero rows
+    // A workgroup looks through 64 groups at a time: those of few tiles are joined a row of lanes each, the others by the
+    // whole workgroup.  Groups without pairs are zero rows.
+    constexpr int64_t kFew = 8;
     for (int64_t u0 = (int64_t)blockIdx.x * kWave; u0 < groups; u0 += (int64_t)gridDim.x * kWave) {
         int64_t a = 0, b = 1;
         if (u0 + lane_id() < groups) {
             a = start_of(g, u0 + lane_id(), pairs);
             b = start_of(g, u0 + lane_id() + 1, pairs);
         }
+        const int64_t t0 = a / g.tile, t1 = b > a ? (b - 1) / g.tile : t0 - 1;
         // the same in every wavefront
-        uint64_t todo = __ballot(b <= a ? !g.group_row : a / kTilePairs != (b - 1) / kTilePairs);
-        while (todo) {
-            const int from = __ffsll((unsigned long long)todo) - 1;
-            todo &= todo - 1;
-            const int64_t ua = __shfl(a, from), ub = __shfl(b, from);
-            const int64_t t0 = ua / kTilePairs, t1 = ub > ua ? (ub - 1) / kTilePairs : -1;
+        const uint64_t few = __ballot(b <= a ? !g.group_row : t1 != t0 && t1 - t0 < kFew);
+        uint64_t many = __ballot(b > a && t1 - t0 >= kFew);
+        for (uint32_t i = row; mine && i < kWave; i += t.rows) {
+            if (!((few >> i) & 1u)) continue;
+            const int64_t ua = start_of(g, u0 + i, pairs), ub = start_of(g, u0 + i + 1, pairs);
+            const int64_t k0 = ua / g.tile, k1 = ub > ua ? (ub - 1) / g.tile : k0 - 1;
+            float sum[VEC] = {};
+            for (int64_t k = k0; k <= k1; ++k) {
+                const Piece<float, VEC> v = load_piece<float, VEC>(g.parts + (k * 2 + (k == k0 ? 1 : 0)) * d + at);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] += v.v[e];
+            }
+            store_group(g, u0 + i, at, sum, out);
+        }
+        while (many) {
+            const int from = __ffsll((unsigned long long)many) - 1;
+            many &= many - 1;
+            const int64_t k0 = __shfl(t0, from), k1 = __shfl(t1, from);
             float sum[VEC] = {};
             if (mine)
-                for (int64_t k = t0 + row; k <= t1; k += t.rows) {
-                    const Piece<float, VEC> v = load_piece<float, VEC>(g.parts + (k * 2 + (k == t0 ? 1 : 0)) * d + at);
+                for (int64_t k = k0 + row; k <= k1; k += t.rows) {
+                    const Piece<float, VEC> v = load_piece<float, VEC>(g.parts + (k * 2 + (k == k0 ? 1 : 0)) * d + at);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[e] += v.v[e];
                 }
@@ -352,13 +377,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
                 for (uint32_t k = 1; k < t.rows; ++k)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[e] += shared[(threadIdx.x + k * t.pieces.d) * VEC + e];
-                const int64_t r = row_of_group(g, u0 + from);
-                if (r >= 0) {
-                    Piece<T, VEC> o;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
-                    store_piece<T, VEC>(out + r * g.out_stride + at, o);
-                }
+                store_group(g, u0 + from, at, sum, out);
             }
         }
     }
@@ -400,11 +419,39 @@ __global__ __launch_bounds__(kThreads) void group_clear_kernel(int32_t d, GroupS
 }
 
 // ------------------------------------------------------------------------------------------------------ launches
+// Pairs of a tile: few enough that 2,048 wavefronts, eight per compute unit, have one, since a tile's rows are fetched
+// eight at a time one after the other; more where there are enough, since a tile leaves up to two rows of floats.
+constexpr int32_t kLeastTile = 8, kMostTile = 64;
+int32_t tile_pairs(int64_t n_pairs, int32_t d, int bytes) {
+    const int vec = d * bytes >= 16 ? 16 / bytes : 1;
+    const int64_t pieces = (d + vec - 1) / vec;
+    int32_t tile = kMostTile;
+    while (tile > kLeastTile && n_pairs / tile * pieces < 2048 * kWave) tile /= 2;
+    return tile;
+}
+
+struct GroupSumPlan {
+    int64_t tiles;
+    size_t o_parts, total;
+};
+GroupSumPlan plan_group_sum(int64_t n_pairs, int32_t d) {
+    GroupSumPlan p;
+    // the type is not known here: as many tiles as the one with the smaller ones has
+    int32_t tile = tile_pairs(n_pairs, d, 2);
+    if (tile_pairs(n_pairs, d, 4) < tile) tile = tile_pairs(n_pairs, d, 4);
+    p.tiles = (n_pairs + tile - 1) / tile;
+    p.o_parts = ((size_t)p.tiles * 4 + 255) / 256 * 256;
+    p.total = p.o_parts + (size_t)p.tiles * 2 * (size_t)d * 4 + 256;
+    return p;
+}
+
+
 template <typename T, typename O, int VEC, bool BY_ROW>
-int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
-                     O* out, hipStream_t stream) {
+int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, GroupSum g, O* out,
+                     hipStream_t stream) {
     const Deal t = make_deal(d, VEC);
-    const int64_t tiles = (g.n_pairs + kTilePairs - 1) / kTilePairs;
+    g.tile = tile_pairs(g.n_pairs, d, (int)sizeof(T));
+    const int64_t tiles = (g.n_pairs + g.tile - 1) / g.tile;
     if (g.n_groups > 0 && tiles > 0) {
         hipLaunchKernelGGL(group_tiles_kernel, dim3((unsigned)((g.n_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
                            stream, g);
@@ -447,20 +494,12 @@ int check_slots(int64_t n, int32_t m, int64_t n_pairs) {
     return ND_OK;
 }
 
-struct GroupSumPlan {
-    int64_t tiles;
-    size_t o_parts, total;
-};
-GroupSumPlan plan_group_sum(int64_t n_pairs, int32_t d) {
-    GroupSumPlan p;
-    p.tiles = (n_pairs + kTilePairs - 1) / kTilePairs;
-    p.o_parts = ((size_t)p.tiles * 4 + 255) / 256 * 256;
-    p.total = p.o_parts + (size_t)p.tiles * 2 * (size_t)d * 4 + 256;
-    return p;
-}
-
 }  // namespace
 
+int64_t group_sum_tiles(int64_t n_pairs, int32_t d, int dtype) {
+    const int32_t tile = tile_pairs(n_pairs, d, (int)dtype_bytes(dtype));
+    return (n_pairs + tile - 1) / tile;
+}
 // Rows of whole pieces only.
 template <typename T>
 int group_sum_floats(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,

@@ -10,6 +10,7 @@
 #include <cfloat>
 #include <type_traits>
 
+#include "nd_philox.h"
 #include "nd_rows.h"
 #include "nd_sweep.h"
 #include "nd_wave.h"
@@ -62,22 +63,28 @@ __global__ __launch_bounds__(kTile) void count_kernel(LossArgs a) {
     }
 }
 
-// Gathers the rows with labels, zeroes what the others get, and pads to a whole tile.
+// Deals out places: rows with labels from the front, the others behind them.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* __restrict__ x, int64_t x_stride,
-                                                          T* __restrict__ rows, T* __restrict__ dx, int64_t dx_stride,
-                                                          int32_t blocks) {
-    __shared__ uint32_t s_before[4], s_all[4], s_bad[4], s_wave[2];
-    __shared__ float s_weight[4];
-    __shared__ int32_t s_row[kTile];
+__global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks) {
+    __shared__ uint32_t s_before[2], s_all[2], s_bad[2], s_wave[2];
+    __shared__ float s_weight[2];
     uint32_t before = 0, all = 0, bad_any = 0;
     float top = 0.f;
-    for (int32_t b = threadIdx.x; b < blocks; b += kThreads) {
-        const uint32_t c = a.block_live[b];
-        all += c;
-        if (b < (int32_t)blockIdx.x) before += c;
-        bad_any |= a.block_bad[b];
-        top = fmaxf(top, a.block_weight[b]);
+    const int64_t row = (int64_t)blockIdx.x * kTile + threadIdx.x;
+    bool bad = false;
+    const int32_t c = row < a.n ? labels_of_row(a, row, &bad) : 0;
+    if (blocks == 1) {  // nothing was counted
+        all = c > 0;
+        bad_any = bad;
+        top = c > 0 ? (a.row_weight ? fabsf(a.row_weight[row]) : 1.f) : 0.f;
+    } else {
+        for (int32_t b = threadIdx.x; b < blocks; b += kTile) {
+            const uint32_t l = a.block_live[b];
+            all += l;
+            if (b < (int32_t)blockIdx.x) before += l;
+            bad_any |= a.block_bad[b];
+            top = fmaxf(top, a.block_weight[b]);
+        }
     }
     for (int s = 32; s > 0; s >>= 1) {
         before += __shfl_xor(before, s);
@@ -85,26 +92,20 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* _
         bad_any |= __shfl_xor(bad_any, s);
         top = fmaxf(top, __shfl_xor(top, s));
     }
+    const uint64_t lives = __ballot(c > 0);
     if (lane_id() == 0) {
         s_before[wave_id()] = before;
         s_all[wave_id()] = all;
         s_bad[wave_id()] = bad_any;
         s_weight[wave_id()] = top;
+        s_wave[wave_id()] = (uint32_t)__popcll(lives);
     }
-    const int64_t row0 = (int64_t)blockIdx.x * kTile;
-    int32_t c = 0;
-    if (threadIdx.x < kTile) {
-        bool bad = false;
-        if (row0 + threadIdx.x < a.n) c = labels_of_row(a, row0 + threadIdx.x, &bad);
-    }
-    const uint64_t lives = __ballot(c > 0);
-    if (threadIdx.x < kTile && lane_id() == 0) s_wave[wave_id()] = (uint32_t)__popcll(lives);
     __syncthreads();
-    before = s_before[0] + s_before[1] + s_before[2] + s_before[3];
-    all = s_all[0] + s_all[1] + s_all[2] + s_all[3];
+    before = s_before[0] + s_before[1];
+    all = s_all[0] + s_all[1];
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        top = fmaxf(fmaxf(s_weight[0], s_weight[1]), fmaxf(s_weight[2], s_weight[3]));
-        a.header->status = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
+        top = fmaxf(s_weight[0], s_weight[1]);
+        a.header->status = s_bad[0] | s_bad[1];
         a.header->n_live = all;
         // fp16 holds 2^-24 to 65,504: the largest product of a weight and a count of labels becomes at most 2^15
         float scale = 1.f;
@@ -112,62 +113,88 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, const T* _
             scale = exp2f(fminf(fmaxf(floorf(log2f(32768.f / (float)a.k) - log2f(top)), -60.f), 60.f));
         a.header->scale = scale;
     }
-    const uint32_t here = s_wave[0] + s_wave[1];
-    if (threadIdx.x < kTile) {
-        const int64_t row = row0 + threadIdx.x;
-        const uint32_t at = (wave_id() == 1 ? s_wave[0] : 0u) + (uint32_t)__popcll(lives & lanes_below(lane_id()));
-        if (c > 0) {
-            s_row[at] = (int32_t)row;
-            a.row_of[before + at] = (int32_t)row;
-            a.count[before + at] = (float)c;
-            a.weight[before + at] = a.row_weight ? a.row_weight[row] : 1.f;
-            for (int32_t j = 0; j < a.k; ++j) {
+    if (row >= a.n) return;
+    // rows with labels in front of this one
+    const int64_t at = before + (wave_id() == 1 ? s_wave[0] : 0u) + (uint32_t)__popcll(lives & lanes_below(lane_id()));
+    if (c > 0) {
+        a.row_of[at] = (int32_t)row;
+        a.count[at] = (float)c;
+        a.weight[at] = a.row_weight ? a.row_weight[row] : 1.f;
+    } else {
+        a.row_of[all + (row - at)] = (int32_t)row;
+    }
+}
+
+// Lanes over places and 16-byte pieces of a padded row.
+struct Spread {
+    FastDiv lanes;   // of a place (at most kThreads)
+    uint32_t places; // of a workgroup
+};
+inline Spread make_spread(int32_t dp, int vec) {
+    const uint32_t pieces = (uint32_t)(dp / vec), lanes = pieces < kThreads ? pieces : kThreads;
+    return Spread{make_fastdiv(lanes), kThreads / lanes};
+}
+inline dim3 spread_grid(const Spread& s, int64_t places) {
+    const int64_t groups = (places + s.places - 1) / s.places;
+    return dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20));
+}
+// A row of d numbers as one of dp, zeros behind.
+template <typename T>
+__device__ __forceinline__ void pad_row(const T* __restrict__ from, T* __restrict__ to, int32_t d, int32_t dp, uint32_t lane,
+                                        uint32_t lanes) {
+    constexpr int VEC = kChunk / (int)sizeof(T);
+    for (int32_t e = (int32_t)lane * VEC; e < dp; e += (int32_t)lanes * VEC) {
+        Piece<T, VEC> v{};
+        if (e + VEC <= d) {
+            v = load_piece<T, VEC>(from + e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (e + i < d) v.v[i] = from[e + i];
+        }
+        store_piece<T, VEC>(to + e, v);
+    }
+}
+
+// The rows with labels one after the other, then zeros up to a whole tile; what rows without labels get.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, Spread s, const T* __restrict__ x, int64_t x_stride,
+                                                          T* __restrict__ rows, T* __restrict__ dx, int64_t dx_stride) {
+    const uint32_t in_group = fastdiv(threadIdx.x, s.lanes), lane = threadIdx.x - in_group * s.lanes.d;
+    if (in_group >= s.places) return;
+    const int64_t live = a.header->n_live, padded = (live + kTile - 1) / kTile * kTile;
+    for (int64_t p = (int64_t)blockIdx.x * s.places + in_group; p < a.n_pad; p += (int64_t)gridDim.x * s.places) {
+        if (p < live) {
+            const int64_t row = a.row_of[p];
+            pad_row(x + row * x_stride, rows + p * a.dp, a.d, a.dp, lane, s.lanes.d);
+            for (int32_t j = (int32_t)lane; j < a.k; j += (int32_t)s.lanes.d) {
                 const int32_t v = a.labels[row * a.k + j];
-                a.labels_of[(int64_t)(before + at) * a.k + j] = v >= 0 && (int64_t)v < a.V ? v : -1;
+                a.labels_of[p * a.k + j] = v >= 0 && (int64_t)v < a.V ? v : -1;
             }
-        } else if (row < a.n) {
-            a.loss[row] = 0.f;
-            a.lse[row] = 0.f;
-            // the places behind the last row that counts have no labels; this row's share of them
-            const int64_t p = all + (row - (before + at));
-            for (int32_t j = 0; j < a.k; ++j) a.labels_of[p * a.k + j] = -1;
+            continue;
         }
-    }
-    __syncthreads();
-    for (uint32_t r = wave_id(); r < here; r += 4) {
-        const T* from = x + (int64_t)s_row[r] * x_stride;
-        T* to = rows + (int64_t)(before + r) * a.dp;
-        for (int32_t e = lane_id(); e < a.dp; e += kWave) to[e] = e < a.d ? from[e] : (T)0.f;
-    }
-    if (dx)  // rows without labels
-        for (int32_t r = wave_id(); r < kTile && row0 + r < a.n; r += 4) {
-            bool dead = true;
-            for (int32_t j = 0; j < a.k; ++j) {
-                const int32_t v = a.labels[(row0 + r) * a.k + j];
-                if (v >= 0 && (int64_t)v < a.V) dead = false;
-            }
-            if (dead)
-                for (int32_t e = lane_id(); e < a.d; e += kWave) dx[(row0 + r) * dx_stride + e] = (T)0.f;
+        if (p < padded) {
+            pad_row((const T*)nullptr, rows + p * a.dp, 0, a.dp, lane, s.lanes.d);
+            if (lane == 0) a.count[p] = a.weight[p] = a.place_lse[p] = 0.f;
         }
-    if ((int32_t)blockIdx.x == blocks - 1) {
-        const uint32_t padded = (all + kTile - 1) / kTile * kTile;
-        for (uint32_t p = all + threadIdx.x; p < padded; p += kThreads) {
-            a.row_of[p] = -1;
-            a.count[p] = 0.f;
-            a.weight[p] = 0.f;
-            a.place_lse[p] = 0.f;
-            for (int32_t j = 0; j < a.k; ++j) a.labels_of[(int64_t)p * a.k + j] = -1;
+        for (int32_t j = (int32_t)lane; j < a.k; j += (int32_t)s.lanes.d) a.labels_of[p * a.k + j] = -1;
+        if (p < a.n) {
+            const int64_t row = a.row_of[p];
+            if (lane == 0) a.loss[row] = a.lse[row] = 0.f;
+            if (dx)
+                for (int32_t e = (int32_t)lane; e < a.d; e += (int32_t)s.lanes.d) dx[row * dx_stride + e] = (T)0.f;
         }
-        for (int64_t e = (int64_t)all * a.dp + threadIdx.x; e < (int64_t)padded * a.dp; e += kThreads) rows[e] = (T)0.f;
     }
 }
 
 // Rows of d numbers at any stride to rows of dp, zeros behind.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void pad_kernel(const T* __restrict__ w, int64_t stride, int64_t rows, int32_t d,
-                                                       int32_t dp, T* __restrict__ out) {
-    for (int64_t r = (int64_t)blockIdx.x * 4 + wave_id(); r < rows; r += (int64_t)gridDim.x * 4)
-        for (int32_t e = lane_id(); e < dp; e += kWave) out[r * dp + e] = e < d ? w[r * stride + e] : (T)0.f;
+                                                       int32_t dp, Spread s, T* __restrict__ out) {
+    const uint32_t in_group = fastdiv(threadIdx.x, s.lanes), lane = threadIdx.x - in_group * s.lanes.d;
+    if (in_group >= s.places) return;
+    for (int64_t r = (int64_t)blockIdx.x * s.places + in_group; r < rows; r += (int64_t)gridDim.x * s.places)
+        pad_row(w + r * stride, out + r * dp, d, dp, lane, s.lanes.d);
 }
 
 // Which row of the sums over labels is a vertex's: none, then those of the groups.
@@ -600,7 +627,7 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
         p.o_parts = take(sums * (size_t)p.dp * 4);
         if (grad) {
             const size_t slots = (size_t)n * (size_t)k, some = slots > 0 ? slots : 1;
-            const size_t tiles = (slots + kTilePairs - 1) / kTilePairs;
+            const size_t tiles = (size_t)group_sum_tiles((int64_t)slots, p.dp, dtype);
             p.label_groups = (int64_t)slots < V ? (int64_t)slots : V;
             p.sort = make_sort_plan((int64_t)slots, V);
             p.o_ctl = take(sizeof(StepCtl));
@@ -716,18 +743,19 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     a.div_k = make_fastdiv((uint32_t)c.k);
     T* rows = (T*)(ws + p.o_rows);
     const unsigned blocks = (unsigned)p.blocks;
-    hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kTile), 0, stream, a);
-    hipLaunchKernelGGL(gather_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, a, (const T*)c.x, c.x_stride, rows,
-                       c.grad ? (T*)c.dx : nullptr, c.dx_stride, (int32_t)blocks);
+    const Spread spread = make_spread(p.dp, kChunk / (int)sizeof(T));
+    if (blocks > 1) hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kTile), 0, stream, a);
+    hipLaunchKernelGGL(place_kernel<T>, dim3(blocks), dim3(kTile), 0, stream, a, (int32_t)blocks);
+    hipLaunchKernelGGL(gather_kernel<T>, spread_grid(spread, p.n_pad), dim3(kThreads), 0, stream, a, spread, (const T*)c.x,
+                       c.x_stride, rows, c.grad ? (T*)c.dx : nullptr, c.dx_stride);
     const T* w = (const T*)c.w;
     int64_t w_stride = c.w_stride;
     // a stride beyond 2^24 numbers would leave 32 bits within a sweep's unit
     const bool as_it_is = c.d == p.dp && w_stride < (1 << 24) && w_stride * (int64_t)sizeof(T) % kChunk == 0 && (uintptr_t)w % kChunk == 0;
     if (!as_it_is) {
         T* padded = (T*)(ws + p.o_w);
-        const int64_t quads = (c.V + 3) / 4;
-        hipLaunchKernelGGL(pad_kernel<T>, dim3((unsigned)(quads < 16384 ? quads : 16384)), dim3(kThreads), 0, stream, w,
-                           w_stride, c.V, c.d, p.dp, padded);
+        hipLaunchKernelGGL(pad_kernel<T>, spread_grid(spread, c.V), dim3(kThreads), 0, stream, w, w_stride, c.V, c.d, p.dp,
+                           spread, padded);
         w = padded;
         w_stride = p.dp;
     }

@@ -416,34 +416,49 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
     }
 }
 
-// Rows of dw whose tile several workgroups had a part of; all of them where there was nothing to sum.
+// Rows of dw whose tile several workgroups had a part of; all of them where there was nothing to sum.  A workgroup takes 32
+// rows of a tile, its lanes four numbers each.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepParts parts, T* __restrict__ dw, int64_t dw_stride) {
-    constexpr int HELD = kSweepHeld;
+    constexpr int HELD = kSweepHeld, kRows = 32, kQuads = D / 4;
     const int64_t live = a.header->n_live;
     const SweepDeal deal(a.V, HELD, live);
     const float back = 1.f / a.header->scale;
-    for (int64_t v = (int64_t)blockIdx.x * 4 + wave_id(); v < a.V; v += (int64_t)gridDim.x * 4) {
+    for (int64_t v0 = (int64_t)blockIdx.x * kRows; v0 < a.V; v0 += (int64_t)gridDim.x * kRows) {
         int64_t x0 = 0, g0 = 0, g1 = -1;
         if (live > 0) {
-            x0 = v / HELD * deal.units;
+            x0 = v0 / HELD * deal.units;
             g0 = deal.group_of(x0);
             g1 = deal.group_of(x0 + deal.units - 1);
             if (g0 == g1) continue;
         }
-        const int32_t labels = live > 0 ? parts.label_row[v] : -1;
-        for (int e = lane_id(); e < a.d; e += kWave) {
-            float sum = 0.f;
+        for (int i = threadIdx.x; i < kRows * kQuads; i += kThreads) {
+            const int64_t v = v0 + i / kQuads;
+            const int e0 = i % kQuads * 4;
+            if (v >= a.V) break;
+            const int32_t labels = live > 0 ? parts.label_row[v] : -1;
+            Float4 sum = {}, less = {};
+            if (labels >= 0) less = *reinterpret_cast<const Float4*>(parts.label_sums + (int64_t)labels * D + e0);
             for (int64_t g = g0; g <= g1; ++g) {
-                const int64_t segment = g * 2 + (deal.first(g) <= x0 ? 1 : 0);
-                sum += parts.rows[(segment * HELD + v % HELD) * D + e];
+                const int64_t segment = g * 2 + (g == g0 && deal.first(g) <= x0 ? 1 : 0);
+                sum += *reinterpret_cast<const Float4*>(parts.rows + (segment * HELD + v % HELD) * D + e0);
             }
-            dw[v * dw_stride + e] = (T)(sum * back - (labels >= 0 ? parts.label_sums[(int64_t)labels * D + e] : 0.f));
+            Piece<T, 4> q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q.v[e] = (T)fmaf(sum[e], back, -less[e]);
+            T* to = dw + v * dw_stride + e0;
+            if (e0 + 4 <= a.d) {
+                store_piece<T, 4>(to, q);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e0 + e < a.d) to[e] = q.v[e];
+            }
         }
     }
 }
 
-// lse, loss and dx of a gathered row, a wavefront each.
+// lse, loss and dx of the gathered rows, a wavefront each at a time; a workgroup's 16 are of one tile.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                           int64_t w_stride, SweepParts parts, T* __restrict__ dx, int64_t dx_stride) {
@@ -451,71 +466,74 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
     constexpr int PER = (D + 63) / 64;  // numbers of a lane: lane, lane + 64, ...
     const int64_t live = a.header->n_live;
     const SweepDeal deal(live, HELD, a.V);
-    for (int64_t p = (int64_t)blockIdx.x * 4 + wave_id(); p < live; p += (int64_t)gridDim.x * 4) {
-        const int64_t tile = p / HELD, x0 = tile * deal.units;
+    constexpr int kRows = 16;
+    for (int64_t p0 = (int64_t)blockIdx.x * kRows; p0 < live; p0 += (int64_t)gridDim.x * kRows) {
+        const int64_t tile = p0 / HELD, x0 = tile * deal.units;
         const int64_t g0 = deal.group_of(x0), g1 = deal.group_of(x0 + deal.units - 1);
-        const int64_t in_tile = p % HELD;
-        float top = -FLT_MAX, sum = 0.f;
-        for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
-            const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile], t = fmaxf(top, t2);
-            sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
-            top = t;
-        }
-        for (int s = 32; s > 0; s >>= 1) {
-            const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s), t = fmaxf(top, t2);
-            sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
-            top = t;
-        }
-        const float lse = top + logf(sum);
-        const int64_t row = a.row_of[p];
-        const float c = a.count[p];
-        float grad[PER] = {}, mine[PER];
-        if (MODE == kSweepDx) {
-            for (int64_t g = g0; g <= g1; ++g) {
-                const int64_t at = (g + tile) * HELD + in_tile;
-                const float f = exp2_of((parts.top[at] - top) * kLog2e);
+        for (int64_t p = p0 + wave_id(); p < p0 + kRows && p < live; p += 4) {
+            const int64_t in_tile = p % HELD;
+            float top = -FLT_MAX, sum = 0.f;
+            for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
+                const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile], t = fmaxf(top, t2);
+                sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
+                top = t;
+            }
+            for (int s = 32; s > 0; s >>= 1) {
+                const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s), t = fmaxf(top, t2);
+                sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
+                top = t;
+            }
+            const float lse = top + logf(sum);
+            const int64_t row = a.row_of[p];
+            const float c = a.count[p];
+            float grad[PER] = {}, mine[PER];
+            if (MODE == kSweepDx) {
+                for (int64_t g = g0; g <= g1; ++g) {
+                    const int64_t at = (g + tile) * HELD + in_tile;
+                    const float f = exp2_of((parts.top[at] - top) * kLog2e);
 #pragma unroll
-                for (int i = 0; i < PER; ++i) grad[i] = fmaf(f, parts.rows[at * D + i * 64 + lane_id()], grad[i]);
+                    for (int i = 0; i < PER; ++i) grad[i] = fmaf(f, parts.rows[at * D + i * 64 + lane_id()], grad[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < PER; ++i) grad[i] *= c / sum;
             }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) grad[i] *= c / sum;
-        }
+            for (int i = 0; i < PER; ++i) mine[i] = (float)rows[p * D + i * 64 + lane_id()];
+            float met = 0.f;
+            for (int32_t j = 0; j < a.k; ++j) {
+                const int32_t v = wave_uniform(a.labels_of[p * a.k + j]);
+                if (v < 0) continue;
+                float dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) mine[i] = (float)rows[p * D + i * 64 + lane_id()];
-        float met = 0.f;
-        for (int32_t j = 0; j < a.k; ++j) {
-            const int32_t v = wave_uniform(a.labels_of[p * a.k + j]);
-            if (v < 0) continue;
-            float dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = i * 64 + lane_id();
-                const float b = (float)w[(int64_t)v * w_stride + e];
-                dot = fmaf(mine[i], b, dot);
-                grad[i] -= b;
+                for (int i = 0; i < PER; ++i) {
+                    const int e = i * 64 + lane_id();
+                    const float b = (float)w[(int64_t)v * w_stride + e];
+                    dot = fmaf(mine[i], b, dot);
+                    grad[i] -= b;
+                }
+                met += dot;
             }
-            met += dot;
-        }
-        for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
-        if (lane_id() == 0) {
-            a.place_lse[p] = lse;
-            a.lse[row] = lse;
-            a.loss[row] = c * lse - met;
-        }
-        if (MODE == kSweepDx) {
-            const float g = a.weight[p];
+            for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
+            if (lane_id() == 0) {
+                a.place_lse[p] = lse;
+                a.lse[row] = lse;
+                a.loss[row] = c * lse - met;
+            }
+            if (MODE == kSweepDx) {
+                const float g = a.weight[p];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = i * 64 + lane_id();
-                if (e < a.d) dx[row * dx_stride + e] = (T)(g * grad[i]);
+                for (int i = 0; i < PER; ++i) {
+                    const int e = i * 64 + lane_id();
+                    if (e < a.d) dx[row * dx_stride + e] = (T)(g * grad[i]);
+                }
             }
         }
     }
 }
 
-// A launch holds fewer than 2^32 lanes: wavefronts go on to further rows from here on.
-inline dim3 wave_per(int64_t rows) {
-    const int64_t groups = (rows + 3) / 4;
+// A launch holds fewer than 2^32 lanes: workgroups go on to further rows from here on.
+inline dim3 groups_for(int64_t rows, int64_t per) {
+    const int64_t groups = (rows + per - 1) / per;
     return dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20));
 }
 
@@ -563,7 +581,7 @@ int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stri
         if (mode == kSweepDx) return launch_sweep<T, D, kSweepDx>(a, s, stream);
         const int rc = launch_sweep<T, D, kSweepDw>(a, s, stream);
         if (rc != ND_OK) return rc;
-        hipLaunchKernelGGL((dw_join_kernel<T, D>), wave_per(a.V), dim3(kThreads), 0, stream, a, parts, dw,
+        hipLaunchKernelGGL((dw_join_kernel<T, D>), groups_for(a.V, 32), dim3(kThreads), 0, stream, a, parts, dw,
                            dw_stride);
         ND_HIP_CHECK(hipGetLastError());
         return ND_OK;
@@ -575,7 +593,7 @@ int sweep_finish(int mode, const LossArgs& a, const T* rows, const T* w, int64_t
                  int64_t dx_stride, hipStream_t stream) {
     return by_width(a.dp, [&](auto width) -> int {
         constexpr int D = decltype(width)::value;
-        const dim3 grid = wave_per(a.n), block(kThreads);
+        const dim3 grid = groups_for(a.n, 16), block(kThreads);
         if (mode == kSweepLse)
             hipLaunchKernelGGL((finish_kernel<T, D, kSweepLse>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx, dx_stride);
         else
