@@ -333,14 +333,17 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
     int32_t at;
     const bool mine = deal_lane<VEC>(t, d, &row, &at);
     const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
-    // A workgroup looks through 64 groups at a time: those of few tiles are joined a row of lanes each, the others by the
-    // whole workgroup.  Groups without pairs are zero rows.
+    // A workgroup looks through 64 groups at a time, from all over the order, since large groups are often neighbours (hubs
+    // have low ids in many graphs): those of few tiles are joined a row of lanes each, the others by the whole workgroup.
+    // Groups without pairs are zero rows.
     constexpr int64_t kFew = 8;
-    for (int64_t u0 = (int64_t)blockIdx.x * kWave; u0 < groups; u0 += (int64_t)gridDim.x * kWave) {
+    const int64_t rounds = (groups + kWave - 1) / kWave;
+    for (int64_t round = blockIdx.x; round < rounds; round += gridDim.x) {
+        const auto group = [&](int64_t i) { return i * rounds + round; };
         int64_t a = 0, b = 1;
-        if (u0 + lane_id() < groups) {
-            a = start_of(g, u0 + lane_id(), pairs);
-            b = start_of(g, u0 + lane_id() + 1, pairs);
+        if (group(lane_id()) < groups) {
+            a = start_of(g, group(lane_id()), pairs);
+            b = start_of(g, group(lane_id()) + 1, pairs);
         }
         const int64_t t0 = a / g.tile, t1 = b > a ? (b - 1) / g.tile : t0 - 1;
         // the same in every wavefront
@@ -348,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
         uint64_t many = __ballot(b > a && t1 - t0 >= kFew);
         for (uint32_t i = row; mine && i < kWave; i += t.rows) {
             if (!((few >> i) & 1u)) continue;
-            const int64_t ua = start_of(g, u0 + i, pairs), ub = start_of(g, u0 + i + 1, pairs);
+            const int64_t ua = start_of(g, group(i), pairs), ub = start_of(g, group(i) + 1, pairs);
             const int64_t k0 = ua / g.tile, k1 = ub > ua ? (ub - 1) / g.tile : k0 - 1;
             float sum[VEC] = {};
             for (int64_t k = k0; k <= k1; ++k) {
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] += v.v[e];
             }
-            store_group(g, u0 + i, at, sum, out);
+            store_group(g, group(i), at, sum, out);
         }
         while (many) {
             const int from = __ffsll((unsigned long long)many) - 1;
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
                 for (uint32_t k = 1; k < t.rows; ++k)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[e] += shared[(threadIdx.x + k * t.pieces.d) * VEC + e];
-                store_group(g, u0 + from, at, sum, out);
+                store_group(g, group(from), at, sum, out);
             }
         }
     }

@@ -458,20 +458,24 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepPart
     }
 }
 
-// lse, loss and dx of the gathered rows, a wavefront each at a time; a workgroup's 16 are of one tile.
+// lse, loss and dx of the gathered rows, a wavefront each at a time; a workgroup's are of one tile.
+constexpr int kFinishRows = 8;
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                           int64_t w_stride, SweepParts parts, T* __restrict__ dx, int64_t dx_stride) {
     constexpr int HELD = kSweepHeld;
-    constexpr int PER = (D + 63) / 64;  // numbers of a lane: lane, lane + 64, ...
+    constexpr int PER = D / 64;     // numbers of a lane
+    constexpr int kAtOnce = 5;      // labels' rows under way
     const int64_t live = a.header->n_live;
     const SweepDeal deal(live, HELD, a.V);
-    constexpr int kRows = 16;
-    for (int64_t p0 = (int64_t)blockIdx.x * kRows; p0 < live; p0 += (int64_t)gridDim.x * kRows) {
+    const int e0 = lane_id() * PER;
+    for (int64_t p0 = (int64_t)blockIdx.x * kFinishRows; p0 < live; p0 += (int64_t)gridDim.x * kFinishRows) {
         const int64_t tile = p0 / HELD, x0 = tile * deal.units;
         const int64_t g0 = deal.group_of(x0), g1 = deal.group_of(x0 + deal.units - 1);
-        for (int64_t p = p0 + wave_id(); p < p0 + kRows && p < live; p += 4) {
-            const int64_t in_tile = p % HELD;
+        for (int64_t p = p0 + wave_id(); p < p0 + kFinishRows && p < live; p += 4) {
+            const int64_t in_tile = p % HELD, row = a.row_of[p];
+            const int32_t my_label = lane_id() < a.k ? a.labels_of[p * a.k + lane_id()] : -1;
+            const Piece<T, PER> x = load_piece<T, PER>(rows + p * D + e0);
             float top = -FLT_MAX, sum = 0.f;
             for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
                 const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile], t = fmaxf(top, t2);
@@ -483,35 +487,38 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
                 sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
                 top = t;
             }
-            const float lse = top + logf(sum);
-            const int64_t row = a.row_of[p];
-            const float c = a.count[p];
-            float grad[PER] = {}, mine[PER];
+            const float lse = top + logf(sum), c = a.count[p];
+            float grad[PER] = {};
             if (MODE == kSweepDx) {
+#pragma unroll 4
                 for (int64_t g = g0; g <= g1; ++g) {
                     const int64_t at = (g + tile) * HELD + in_tile;
                     const float f = exp2_of((parts.top[at] - top) * kLog2e);
+                    const Piece<float, PER> v = load_piece<float, PER>(parts.rows + at * D + e0);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) grad[i] = fmaf(f, parts.rows[at * D + i * 64 + lane_id()], grad[i]);
+                    for (int i = 0; i < PER; ++i) grad[i] = fmaf(f, v.v[i], grad[i]);
                 }
 #pragma unroll
                 for (int i = 0; i < PER; ++i) grad[i] *= c / sum;
             }
-#pragma unroll
-            for (int i = 0; i < PER; ++i) mine[i] = (float)rows[p * D + i * 64 + lane_id()];
             float met = 0.f;
-            for (int32_t j = 0; j < a.k; ++j) {
-                const int32_t v = wave_uniform(a.labels_of[p * a.k + j]);
-                if (v < 0) continue;
-                float dot = 0.f;
+            for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
+                Piece<T, PER> r[kAtOnce];
+                int32_t v[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int e = i * 64 + lane_id();
-                    const float b = (float)w[(int64_t)v * w_stride + e];
-                    dot = fmaf(mine[i], b, dot);
-                    grad[i] -= b;
+                for (int j = 0; j < kAtOnce; ++j) {
+                    v[j] = j0 + j < a.k ? __builtin_amdgcn_readlane(my_label, j0 + j) : -1;
+                    r[j] = Piece<T, PER>{};
+                    if (v[j] >= 0) r[j] = load_piece<T, PER>(w + (int64_t)v[j] * w_stride + e0);
                 }
-                met += dot;
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        if (v[j] < 0) continue;
+                        met = fmaf((float)x.v[i], (float)r[j].v[i], met);
+                        grad[i] -= (float)r[j].v[i];
+                    }
             }
             for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
             if (lane_id() == 0) {
@@ -521,10 +528,16 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
             }
             if (MODE == kSweepDx) {
                 const float g = a.weight[p];
+                Piece<T, PER> o;
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int e = i * 64 + lane_id();
-                    if (e < a.d) dx[row * dx_stride + e] = (T)(g * grad[i]);
+                for (int i = 0; i < PER; ++i) o.v[i] = (T)(g * grad[i]);
+                T* to = dx + row * dx_stride + e0;
+                if (e0 + PER <= a.d) {
+                    store_piece<T, PER>(to, o);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if (e0 + i < a.d) to[i] = o.v[i];
                 }
             }
         }
@@ -593,7 +606,7 @@ int sweep_finish(int mode, const LossArgs& a, const T* rows, const T* w, int64_t
                  int64_t dx_stride, hipStream_t stream) {
     return by_width(a.dp, [&](auto width) -> int {
         constexpr int D = decltype(width)::value;
-        const dim3 grid = groups_for(a.n, 16), block(kThreads);
+        const dim3 grid = groups_for(a.n, kFinishRows), block(kThreads);
         if (mode == kSweepLse)
             hipLaunchKernelGGL((finish_kernel<T, D, kSweepLse>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx, dx_stride);
         else
