@@ -19,9 +19,8 @@ namespace nd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;         // rows and columns of a product's tile
+constexpr int kTile = 128;         // rows of a product's tile
 constexpr int kChunk = 16;         // bytes that a lane moves at once
-constexpr int kTileBytes = kTile * 128;  // one operand's tile: 128 bytes of the summed dimension
 constexpr size_t kPieceBytes = 512u << 20;  // probabilities that lie in the workspace at a time
 
 typedef float Acc __attribute__((ext_vector_type(16)));
@@ -209,10 +208,11 @@ __global__ __launch_bounds__(kThreads) void label_rows_kernel(const StepCtl* __r
 }
 
 // ------------------------------------------------------------------------------------------------ product of tiles
-// C[m][n] = sum_k A(m, k) B(n, k) for a tile of 128 x 128, four wavefronts of 64 x 64 each in 32 x 32 matrix
-// instructions.  An operand lies in memory with the summed dimension along its rows (ACROSS = false) or down its columns
-// (ACROSS = true), and in LDS as it does in memory, 16-byte pieces of a row exchanged so that the reads of a
-// wavefront fall on different banks.
+// C[m][n] = sum_k A(m, k) B(n, k) for a tile of 256 x 128, four wavefronts of 128 x 64 each in 32 x 32 matrix
+// instructions: eight of them use six operands, so that LDS, which gives a wavefront's operand of 1 KB in 5 to 9 cycles
+// (transposed reads) and has four SIMDs to feed, keeps ahead of them.  An operand lies in memory with the summed
+// dimension along its rows (ACROSS = false) or down its columns (ACROSS = true), and in LDS as it does in memory, 16-byte
+// pieces of a row exchanged so that the reads of a wavefront fall on different banks.
 template <typename T>
 struct Operand {
     const T* base;
@@ -221,47 +221,67 @@ struct Operand {
     int32_t cols;   // ACROSS: numbers in a row (a multiple of a piece): pieces behind are the last one again
 };
 
+constexpr int kTileM = 256, kTileN = 128;
+constexpr int kStepBytes = 64;                               // of the summed dimension at a time
+constexpr int kLdsM = kTileM * kStepBytes, kLdsN = kTileN * kStepBytes, kLdsBytes = 2 * (kLdsM + kLdsN);
+
 template <typename T>
 struct Kind {
     static constexpr int kVec = kChunk / (int)sizeof(T);       // numbers in a piece
-    static constexpr int kStep = 128 / (int)sizeof(T);         // of the summed dimension in a tile
+    static constexpr int kStep = kStepBytes / (int)sizeof(T);  // of the summed dimension in a tile
     static constexpr bool kWide = sizeof(T) == 4;
 };
 
-// Byte position of piece c of row r in LDS.
-template <typename T, bool ACROSS>
+// Byte position in LDS of piece c of row r of a tile SIZE wide: SIZE rows of 4 pieces, or kStep rows of SIZE numbers.
+template <typename T, bool ACROSS, int SIZE>
 __device__ __forceinline__ int lds_place(int r, int c) {
-    if (!ACROSS) return (r * 8 + (c ^ ((r >> 1) & 7))) * kChunk;                               // 128 rows of 8 pieces
-    if (Kind<T>::kWide) return (r * 32 + (c ^ (((r >> 2) & 1) << 3))) * kChunk;                // 32 rows of 32 pieces
-    return (r * 16 + (c ^ (((r & 3) << 2) | ((r >> 2) & 3)))) * kChunk;                        // 64 rows of 16 pieces
+    if (!ACROSS) return (r * 4 + (c ^ ((r >> 2) & 3))) * kChunk;
+    constexpr int kPieces = SIZE / Kind<T>::kVec;
+    if (Kind<T>::kWide) return (r * kPieces + (c ^ (((r >> 2) & 1) << 3))) * kChunk;
+    return (r * kPieces + (c ^ (((r & 3) << 2) | ((r >> 2) & 3)))) * kChunk;
 }
 
 typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
-struct Chunks {
-    Word4 v[4];
+
+// A lane's pieces of an operand's tile, on their way to LDS.
+template <typename T, bool ACROSS, int SIZE>
+struct Mover {
+    static constexpr int kCount = SIZE * kStepBytes / (kThreads * kChunk);
+    static constexpr int kPieces = ACROSS ? SIZE / Kind<T>::kVec : 4;  // of a row of the tile
+    Word4 v[kCount];
+    const T* at[kCount];   // not ACROSS: the lane's rows; ACROSS: the lane's columns
+    __device__ __forceinline__ Mover(const Operand<T>& o, int64_t m0) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int e = i * kThreads + (int)threadIdx.x, r = e / kPieces, p = e % kPieces;
+            if (!ACROSS) {
+                const int64_t row = m0 + r < o.rows ? m0 + r : o.rows - 1;
+                at[i] = o.base + row * o.stride + p * Kind<T>::kVec;
+            } else {
+                const int64_t col = m0 + p * Kind<T>::kVec, last = o.cols - Kind<T>::kVec;
+                at[i] = o.base + (col < last ? col : last);
+            }
+        }
+    }
+    __device__ __forceinline__ void fetch(const Operand<T>& o, int64_t k) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            if (!ACROSS) {
+                v[i] = *reinterpret_cast<const Word4*>(at[i] + k);
+            } else {
+                const int64_t r = k + (i * kThreads + (int)threadIdx.x) / kPieces;
+                v[i] = *reinterpret_cast<const Word4*>(at[i] + (r < o.rows ? r : o.rows - 1) * o.stride);
+            }
+        }
+    }
+    __device__ __forceinline__ void keep(char* lds) const {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int e = i * kThreads + (int)threadIdx.x;
+            *reinterpret_cast<Word4*>(lds + lds_place<T, ACROSS, SIZE>(e / kPieces, e % kPieces)) = v[i];
+        }
+    }
 };
-template <typename T, bool ACROSS>
-__device__ __forceinline__ void fetch(const Operand<T>& o, int64_t m0, int64_t k0, Chunks& c) {
-    constexpr int kPieces = ACROSS ? kTile / Kind<T>::kVec : 8;  // of a row of the tile
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int e = i * kThreads + (int)threadIdx.x, r = e / kPieces, p = e % kPieces;
-        int64_t row = (ACROSS ? k0 : m0) + r;
-        row = row < o.rows ? row : o.rows - 1;
-        int64_t col = (ACROSS ? m0 : k0) + p * Kind<T>::kVec;
-        if (ACROSS && col > o.cols - Kind<T>::kVec) col = o.cols - Kind<T>::kVec;
-        c.v[i] = *reinterpret_cast<const Word4*>(o.base + row * o.stride + col);
-    }
-}
-template <typename T, bool ACROSS>
-__device__ __forceinline__ void keep(char* lds, const Chunks& c) {
-    constexpr int kPieces = ACROSS ? kTile / Kind<T>::kVec : 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int e = i * kThreads + (int)threadIdx.x;
-        *reinterpret_cast<Word4*>(lds + lds_place<T, ACROSS>(e / kPieces, e % kPieces)) = c.v[i];
-    }
-}
 
 // A lane's share of a 32-row block for one group of the summed dimension: 16-bit types 16 of it, lane l holds row l % 32
 // and the eight from 8 (l / 32) on; fp32 8 of it, the four from 4 (l / 32) on, one for each of four instructions.
@@ -269,25 +289,25 @@ template <typename T>
 struct Fragment {
     T v[Kind<T>::kVec];
 };
-template <typename T, bool ACROSS>
+template <typename T, bool ACROSS, int SIZE>
 __device__ __forceinline__ Fragment<T> fragment(const char* lds, int block_row, int group) {
     const int lane = lane_id(), half = lane >> 5;
     Fragment<T> f;
     if (!ACROSS) {
         const int r = block_row + (lane & 31);
-        f = *reinterpret_cast<const Fragment<T>*>(lds + lds_place<T, false>(r, group * 2 + half));
+        f = *reinterpret_cast<const Fragment<T>*>(lds + lds_place<T, false, SIZE>(r, group * 2 + half));
     } else if (Kind<T>::kWide) {
         const int col = block_row + (lane & 31);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            f.v[e] = *reinterpret_cast<const T*>(lds + lds_place<T, true>(group * 8 + half * 4 + e, col / 4) + col % 4 * 4);
+            f.v[e] = *reinterpret_cast<const T*>(lds + lds_place<T, true, SIZE>(group * 8 + half * 4 + e, col / 4) + col % 4 * 4);
     } else {
         // 16 lanes hand in 4 rows x 16 columns and get a column of four rows each
         const int sub = lane & 15, col = block_row + ((lane >> 4) & 1) * 16 + (sub & 3) * 4;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = group * 16 + half * 8 + e * 4 + (sub >> 2);
-            const char* at = lds + lds_place<T, true>(r, col / 8) + (col & 4) * 2;
+            const char* at = lds + lds_place<T, true, SIZE>(r, col / 8) + (col & 4) * 2;
             const Short4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) Short4*)at);
             __builtin_memcpy(&f.v[e * 4], &t, 8);
@@ -315,43 +335,43 @@ __device__ __forceinline__ Acc multiply(const Fragment<f16_t>& a, const Fragment
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
 }
 
-// The tile at (m0, n0) summed over [k0, k1), k1 - k0 a multiple of Kind::kStep; lds: 4 * kTileBytes.  Ends with a barrier.
-// Result: lane l of wavefront w holds column n = 64 (w % 2) + 32 j + l % 32 and rows m = 64 (w / 2) + 32 i + 8 (r / 4) +
+// The tile at (m0, n0) summed over [k0, k1), k1 - k0 a multiple of Kind::kStep; lds: kLdsBytes.  Ends with a barrier.
+// Result: lane l of wavefront w holds column n = 64 (w % 2) + 32 j + l % 32 and rows m = 128 (w / 2) + 32 i + 8 (r / 4) +
 // 4 (l / 32) + r % 4 in acc[i][j][r].
+typedef Acc AccTile[4][2];
 template <typename T, bool A_ACROSS, bool B_ACROSS>
 __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0, int64_t k0,
-                                        int64_t k1, char* lds, Acc (&acc)[2][2]) {
-    constexpr int kGroups = Kind<T>::kWide ? 4 : 4;  // 32 / 8, 64 / 16
-    const int wm = wave_id() / 2 * 64, wn = wave_id() % 2 * 64;
+                                        int64_t k1, char* lds, AccTile& acc) {
+    const int wm = wave_id() / 2 * 128, wn = wave_id() % 2 * 64;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[i][j] = Acc{};
     if (k0 >= k1) return;
-    Chunks ca, cb;
-    fetch<T, A_ACROSS>(a, m0, k0, ca);
-    fetch<T, B_ACROSS>(b, n0, k0, cb);
+    Mover<T, A_ACROSS, kTileM> ma(a, m0);
+    Mover<T, B_ACROSS, kTileN> mb(b, n0);
+    ma.fetch(a, k0);
+    mb.fetch(b, k0);
     int buffer = 0;
     for (int64_t k = k0; k < k1; k += Kind<T>::kStep) {
-        char* la = lds + buffer * 2 * kTileBytes;
-        char* lb = la + kTileBytes;
-        keep<T, A_ACROSS>(la, ca);
-        keep<T, B_ACROSS>(lb, cb);
+        char* la = lds + buffer * (kLdsM + kLdsN);
+        char* lb = la + kLdsM;
+        ma.keep(la);
+        mb.keep(lb);
         __syncthreads();
         if (k + Kind<T>::kStep < k1) {
-            fetch<T, A_ACROSS>(a, m0, k + Kind<T>::kStep, ca);
-            fetch<T, B_ACROSS>(b, n0, k + Kind<T>::kStep, cb);
+            ma.fetch(a, k + Kind<T>::kStep);
+            mb.fetch(b, k + Kind<T>::kStep);
         }
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            Fragment<T> fa[2], fb[2];
+        for (int g = 0; g < 2; ++g) {
+            Fragment<T> fa[4], fb[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = fragment<T, A_ACROSS>(la, wm + i * 32, g);
-                fb[i] = fragment<T, B_ACROSS>(lb, wn + i * 32, g);
-            }
+            for (int j = 0; j < 2; ++j) fb[j] = fragment<T, B_ACROSS, kTileN>(lb, wn + j * 32, g);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 4; ++i) fa[i] = fragment<T, A_ACROSS, kTileM>(la, wm + i * 32, g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fa[i], fb[j], acc[i][j]);
         }
@@ -359,36 +379,43 @@ __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b
     }
     __syncthreads();
 }
-__device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 64 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
+__device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 128 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
 __device__ __forceinline__ int acc_col(int j) { return wave_id() % 2 * 64 + j * 32 + (lane_id() & 31); }
 
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // ------------------------------------------------------------------------------------------------------- forward
-// A workgroup takes 128 rows and every groups-th tile of vertices; a lane keeps maximum and sum of its two columns.
+// A workgroup takes 128 rows and every groups-th tile of 256 vertices; a lane keeps maximum and sum of its two columns.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x) {
-    __shared__ __align__(16) char lds[4 * kTileBytes];
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x) {
+    __shared__ __align__(16) char lds[kLdsBytes];
     const int64_t n0 = (int64_t)blockIdx.x * kTile;
     if (n0 >= (int64_t)a.header->n_live) return;
     float top[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {};
-    for (int64_t v0 = (int64_t)blockIdx.y * kTile; v0 < a.V; v0 += (int64_t)a.groups * kTile) {
-        Acc acc[2][2];
+    for (int64_t v0 = (int64_t)blockIdx.y * kTileM; v0 < a.V; v0 += (int64_t)a.groups * kTileM) {
+        AccTile acc;
         product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
+        if (a.V - v0 < kTileM) {  // behind the last vertex
+            const int left = (int)(a.V - v0) - acc_row(0, 0);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (i * 32 + 8 * (r / 4) + r % 4 >= left) acc[i][j][r] = -INFINITY;
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float t = top[j];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (v0 + acc_row(i, r) >= a.V) acc[i][j][r] = -INFINITY;
-                    t = fmaxf(t, acc[i][j][r]);
-                }
+                for (int r = 0; r < 16; ++r) t = fmaxf(t, acc[i][j][r]);
             float s = sum[j] * exp_of(top[j] - t);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s += exp_of(acc[i][j][r] - t);
             top[j] = t;
@@ -457,24 +484,24 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __r
 }
 
 // ------------------------------------------------------------------------------------------------------ gradient
-// g (c p - count) of 128 vertices of the piece from v_first on and 128 rows, as [vertex][row].
+// g (c p - count) of 256 vertices of the piece from v_first on and 128 rows, as [vertex][row].
 template <typename T>
-__global__ __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
                                                          T* __restrict__ probs) {
-    __shared__ __align__(16) char lds[4 * kTileBytes];
-    constexpr int kPitch = kTile + 4;
-    const int64_t n0 = (int64_t)blockIdx.x * kTile, v0 = v_first + (int64_t)blockIdx.y * kTile;
+    __shared__ __align__(16) char lds[kLdsBytes];
+    constexpr int kPitch = kTileM + 4;
+    const int64_t n0 = (int64_t)blockIdx.x * kTile, v0 = v_first + (int64_t)blockIdx.y * kTileM;
     if (n0 >= (int64_t)a.header->n_live) return;
-    Acc acc[2][2];
+    AccTile acc;
     product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
-    // how often a vertex is among a row's labels: a lane owns a row's 128 counts
+    // how often a vertex is among a row's labels: a lane owns a row's 256 counts
     uint8_t* counts = reinterpret_cast<uint8_t*>(lds);
     if (threadIdx.x < kTile) {
         uint32_t* mine = reinterpret_cast<uint32_t*>(counts + threadIdx.x * kPitch);
-        for (int e = 0; e < kTile / 4; ++e) mine[e] = 0;
+        for (int e = 0; e < kTileM / 4; ++e) mine[e] = 0;
         for (int32_t j = 0; j < a.k; ++j) {
             const int64_t v = a.labels_of[(n0 + threadIdx.x) * a.k + j];
-            if (v >= v0 && v < v0 + kTile) counts[threadIdx.x * kPitch + (v - v0)]++;
+            if (v >= v0 && v < v0 + kTileM) counts[threadIdx.x * kPitch + (v - v0)]++;
         }
     }
     __syncthreads();
@@ -484,63 +511,88 @@ __global__ __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> 
         const int col = acc_col(j);
         const float lse = a.place_lse[n0 + col], c = a.count[n0 + col], g = a.weight[n0 + col] * scale;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int row = acc_row(i, r);
                 const float held = (float)counts[col * kPitch + row];
                 const float p = v0 + row < a.V && c > 0.f ? g * (c * exp_of(acc[i][j][r] - lse) - held) : 0.f;
-                probs[((int64_t)blockIdx.y * kTile + row) * a.n_pad + n0 + col] = (T)p;
+                probs[((int64_t)blockIdx.y * kTileM + row) * a.n_pad + n0 + col] = (T)p;
             }
     }
 }
 
-// dw of 128 vertices of the piece and 128 numbers of their rows.
+// dw of 256 vertices of the piece and 128 numbers of their rows, over a share of the rows with labels: the result where
+// there is one share, else its part.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
-                                                      T* __restrict__ dw, int64_t dw_stride) {
-    __shared__ __align__(16) char lds[4 * kTileBytes];
-    const int64_t m0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTile;
-    const int64_t live = a.header->n_live, k1 = (live + Kind<T>::kStep - 1) / Kind<T>::kStep * Kind<T>::kStep;
-    Acc acc[2][2];
-    product<T, false, true>(probs, x, m0, d0, 0, k1, lds, acc);
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
+                                                      T* __restrict__ dw, int64_t dw_stride, float* __restrict__ parts,
+                                                      int64_t part_rows) {
+    __shared__ __align__(16) char lds[kLdsBytes];
+    const int64_t m0 = (int64_t)blockIdx.x * kTileM, d0 = (int64_t)blockIdx.y * kTileN;
+    const int64_t steps = ((int64_t)a.header->n_live + Kind<T>::kStep - 1) / Kind<T>::kStep;
+    const int64_t k0 = steps * blockIdx.z / gridDim.z * Kind<T>::kStep, k1 = steps * (blockIdx.z + 1) / gridDim.z * Kind<T>::kStep;
+    AccTile acc;
+    product<T, false, true>(probs, x, m0, d0, k0, k1, lds, acc);
     const float back = 1.f / a.header->scale;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+        const int64_t e = d0 + acc_col(j);
+        if (e >= a.d) continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int64_t v = v_first + m0 + acc_row(i, r), e = d0 + acc_col(j);
-                if (v < a.V && e < a.d) dw[v * dw_stride + e] = (T)(acc[i][j][r] * back);
+                const int64_t m = m0 + acc_row(i, r);
+                if (v_first + m >= a.V) continue;
+                if (gridDim.z == 1)
+                    dw[(v_first + m) * dw_stride + e] = (T)(acc[i][j][r] * back);
+                else
+                    parts[((int64_t)blockIdx.z * part_rows + m) * a.dp + e] = acc[i][j][r];
             }
+    }
+}
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
+                                                           int64_t part_rows, int64_t v_first, int64_t here, T* __restrict__ dw,
+                                                           int64_t dw_stride) {
+    const float back = 1.f / a.header->scale;
+    for (int64_t m = (int64_t)blockIdx.x * 4 + wave_id(); m < here; m += (int64_t)gridDim.x * 4)
+        for (int32_t e = lane_id(); e < a.d; e += kWave) {
+            float sum = 0.f;
+#pragma unroll 4
+            for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * part_rows + m) * a.dp + e];
+            dw[(v_first + m) * dw_stride + e] = (T)(sum * back);
+        }
 }
 
-// dx of 128 rows and 128 numbers, summed over a share of the piece's vertices.
+// dx of 256 numbers of 128 rows, summed over a share of the piece's vertices.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
                                                       int64_t v_share, int64_t v_end, int first_piece,
                                                       float* __restrict__ parts) {
-    __shared__ __align__(16) char lds[4 * kTileBytes];
-    const int64_t n0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTile;
+    __shared__ __align__(16) char lds[kLdsBytes];
+    const int64_t n0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTileM;
     if (n0 >= (int64_t)a.header->n_live) return;
     const int64_t k0 = (int64_t)blockIdx.z * v_share;
     const int64_t k1 = k0 + v_share < v_end ? k0 + v_share : v_end;
     Operand<T> piece = w;
     piece.base += v_first * w.stride;
     piece.rows -= v_first;
-    Acc acc[2][2];
-    product<T, true, true>(probs, piece, n0, d0, k0, k1, lds, acc);
+    AccTile acc;
+    product<T, true, true>(piece, probs, d0, n0, k0, k1, lds, acc);
+    typedef float Float4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t e = d0 + acc_col(j);
+            for (int r = 0; r < 16; r += 4) {
+                const int64_t e = d0 + acc_row(i, r);
                 if (e >= a.dp) continue;
-                float* at = parts + ((int64_t)blockIdx.z * a.n_pad + n0 + acc_row(i, r)) * a.dp + e;
-                *at = first_piece ? acc[i][j][r] : *at + acc[i][j][r];
+                Float4* at = reinterpret_cast<Float4*>(parts + ((int64_t)blockIdx.z * a.n_pad + n0 + acc_col(j)) * a.dp + e);
+                const Float4 v = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+                *at = first_piece ? v : *at + v;
             }
 }
 
@@ -569,13 +621,13 @@ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct LossPlan {
     int64_t n_pad, blocks, piece;   // piece: vertices at a time (a multiple of a tile)
-    int32_t dp, groups, shares;
+    int32_t dp, groups, shares, dw_shares;
     bool sweep;                     // rows short enough for nd_sweep.hip
     // labels by vertex: the grouping's arrays, sums of their rows
     int64_t label_groups;
     SortPlan sort;
     size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group, o_label_parts;
-    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, total;
+    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, o_dw_parts, total;
 };
 LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool grad) {
     LossPlan p{};
@@ -584,20 +636,23 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     p.dp = p.sweep ? sweep_width(d) : (int32_t)((d + step - 1) / step * step);
     p.blocks = n > 0 ? (n + kTile - 1) / kTile : 1;  // without rows: the header is written all the same
     p.n_pad = p.blocks * kTile;
-    const int64_t v_tiles = (V + kTile - 1) / kTile;
+    const int64_t v_tiles = (V + kTileM - 1) / kTileM;
     // enough workgroups to fill the chip several times over
     const int64_t groups = (1024 + p.blocks - 1) / p.blocks;
     p.groups = (int32_t)(groups < v_tiles ? groups : v_tiles);
-    int64_t piece_tiles = (int64_t)(kPieceBytes / (size_t)(p.n_pad * kTile * b));
+    int64_t piece_tiles = (int64_t)(kPieceBytes / (size_t)(p.n_pad * kTileM * b));
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > 32768) piece_tiles = 32768;
     if (piece_tiles > v_tiles) piece_tiles = v_tiles;
-    p.piece = piece_tiles * kTile;
-    const int64_t dx_tiles = p.blocks * ((p.dp + kTile - 1) / kTile);
-    int64_t shares = (512 + dx_tiles - 1) / dx_tiles;
-    if (shares > 16) shares = 16;
-    if (shares > piece_tiles) shares = piece_tiles;
-    p.shares = (int32_t)shares;
+    p.piece = piece_tiles * kTileM;
+    // the summed dimension is shared out where there are fewer tiles than two per compute unit
+    auto shares = [](int64_t tiles, int64_t most) {
+        int64_t s = (512 + tiles - 1) / tiles;
+        s = s < 16 ? s : 16;
+        return (int32_t)(s < most ? s : most);
+    };
+    p.shares = shares(p.blocks * ((p.dp + kTileM - 1) / kTileM), piece_tiles);
+    p.dw_shares = shares(piece_tiles * ((p.dp + kTileN - 1) / kTileN), p.blocks);
     size_t o = sizeof(LossHeader);
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -652,6 +707,7 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     if (grad) {
         p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
         p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
+        p.o_dw_parts = p.dw_shares > 1 ? take((size_t)p.dw_shares * (size_t)p.piece * (size_t)p.dp * 4) : 0;
     }
     p.total = o;
     return p;
@@ -780,19 +836,22 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     if (c.grad) {
         T* probs = (T*)(ws + p.o_probs);
         float* parts = (float*)(ws + p.o_parts);
-        const unsigned d_tiles = (unsigned)((p.dp + kTile - 1) / kTile);
+        float* dw_parts = (float*)(ws + p.o_dw_parts);
         for (int64_t v = 0; v < c.V; v += p.piece) {
-            const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTile - 1) / kTile;
-            const Operand<T> op{probs, p.n_pad, tiles * kTile, (int32_t)p.n_pad};
+            const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTileM - 1) / kTileM;
+            const Operand<T> op{probs, p.n_pad, tiles * kTileM, (int32_t)p.n_pad};
             if (c.n > 0)
                 hipLaunchKernelGGL(probs_kernel<T>, dim3(blocks, (unsigned)tiles), dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)
-                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)tiles, d_tiles), dim3(kThreads), 0, stream, a, op, ox, v,
-                                   (T*)c.dw, c.dw_stride);
+                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)tiles, (unsigned)((p.dp + kTileN - 1) / kTileN), (unsigned)p.dw_shares),
+                                   dim3(kThreads), 0, stream, a, op, ox, v, (T*)c.dw, c.dw_stride, dw_parts, p.piece);
+            if (c.dw && p.dw_shares > 1)
+                hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
+                                   here, (T*)c.dw, c.dw_stride);
             if (c.dx && c.n > 0) {
-                const int64_t share = (tiles + p.shares - 1) / p.shares * kTile;
-                hipLaunchKernelGGL(dx_kernel<T>, dim3(blocks, d_tiles, (unsigned)p.shares), dim3(kThreads), 0, stream, a, op, ow,
-                                   v, share, tiles * kTile, (int)(v == 0), parts);
+                const int64_t share = (tiles + p.shares - 1) / p.shares * kTileM;
+                hipLaunchKernelGGL(dx_kernel<T>, dim3(blocks, (unsigned)((p.dp + kTileM - 1) / kTileM), (unsigned)p.shares), dim3(kThreads), 0, stream, a, op, ow,
+                                   v, share, tiles * kTileM, (int)(v == 0), parts);
             }
         }
         if (c.dx && c.n > 0)
