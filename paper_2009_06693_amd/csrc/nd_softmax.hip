@@ -248,8 +248,9 @@ template <typename T, bool ACROSS, int SIZE>
 struct Mover {
     static constexpr int kCount = SIZE * kStepBytes / (kThreads * kChunk);
     static constexpr int kPieces = ACROSS ? SIZE / Kind<T>::kVec : 4;  // of a row of the tile
-    Word4 v[kCount];
-    const T* at[kCount];   // not ACROSS: the lane's rows; ACROSS: the lane's columns
+    Word4 v[2][kCount];    // two steps are under way
+    const T* at[ACROSS ? 1 : kCount];       // the lane's rows,
+    int32_t column[ACROSS ? kCount : 1];    // or its columns
     __device__ __forceinline__ Mover(const Operand<T>& o, int64_t m0) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
@@ -259,26 +260,31 @@ struct Mover {
                 at[i] = o.base + row * o.stride + p * Kind<T>::kVec;
             } else {
                 const int64_t col = m0 + p * Kind<T>::kVec, last = o.cols - Kind<T>::kVec;
-                at[i] = o.base + (col < last ? col : last);
+                column[i] = (int32_t)(col < last ? col : last);
             }
         }
     }
+    template <int SET>
     __device__ __forceinline__ void fetch(const Operand<T>& o, int64_t k) {
+        const int64_t k_row = k < o.rows ? k : o.rows - 1;
+        const uint32_t left = o.rows - k_row < Kind<T>::kStep ? (uint32_t)(o.rows - k_row) : (uint32_t)Kind<T>::kStep;
+        const T* across = o.base + k_row * o.stride;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             if (!ACROSS) {
-                v[i] = *reinterpret_cast<const Word4*>(at[i] + k);
+                v[SET][i] = *reinterpret_cast<const Word4*>(at[i] + k);
             } else {
-                const int64_t r = k + (i * kThreads + (int)threadIdx.x) / kPieces;
-                v[i] = *reinterpret_cast<const Word4*>(at[i] + (r < o.rows ? r : o.rows - 1) * o.stride);
+                const uint32_t r = ((uint32_t)(i * kThreads) + threadIdx.x) / kPieces;
+                v[SET][i] = *reinterpret_cast<const Word4*>(across + ((uint64_t)(r < left ? r : left - 1u) * (uint32_t)o.stride + (uint32_t)column[i]));
             }
         }
     }
+    template <int SET>
     __device__ __forceinline__ void keep(char* lds) const {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int e = i * kThreads + (int)threadIdx.x;
-            *reinterpret_cast<Word4*>(lds + lds_place<T, ACROSS, SIZE>(e / kPieces, e % kPieces)) = v[i];
+            *reinterpret_cast<Word4*>(lds + lds_place<T, ACROSS, SIZE>(e / kPieces, e % kPieces)) = v[SET][i];
         }
     }
 };
@@ -335,6 +341,13 @@ __device__ __forceinline__ Acc multiply(const Fragment<f16_t>& a, const Fragment
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
 }
 
+// A barrier for what lies in LDS only: loads from memory stay under way across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // The tile at (m0, n0) summed over [k0, k1), k1 - k0 a multiple of Kind::kStep; lds: kLdsBytes.  Ends with a barrier.
 // Result: lane l of wavefront w holds column n = 64 (w % 2) + 32 j + l % 32 and rows m = 128 (w / 2) + 32 i + 8 (r / 4) +
 // 4 (l / 32) + r % 4 in acc[i][j][r].
@@ -350,19 +363,22 @@ __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b
     if (k0 >= k1) return;
     Mover<T, A_ACROSS, kTileM> ma(a, m0);
     Mover<T, B_ACROSS, kTileN> mb(b, n0);
-    ma.fetch(a, k0);
-    mb.fetch(b, k0);
-    int buffer = 0;
-    for (int64_t k = k0; k < k1; k += Kind<T>::kStep) {
-        char* la = lds + buffer * (kLdsM + kLdsN);
+    constexpr int kStep = Kind<T>::kStep;
+    const int64_t last = k1 - kStep;  // behind it the last step is fetched again
+    ma.template fetch<0>(a, k0);
+    mb.template fetch<0>(b, k0);
+    ma.template fetch<1>(a, k0 < last ? k0 + kStep : last);
+    mb.template fetch<1>(b, k0 < last ? k0 + kStep : last);
+    auto step = [&](int64_t k, auto set) {
+        constexpr int SET = decltype(set)::value;
+        char* la = lds + SET * (kLdsM + kLdsN);
         char* lb = la + kLdsM;
-        ma.keep(la);
-        mb.keep(lb);
-        __syncthreads();
-        if (k + Kind<T>::kStep < k1) {
-            ma.fetch(a, k + Kind<T>::kStep);
-            mb.fetch(b, k + Kind<T>::kStep);
-        }
+        ma.template keep<SET>(la);
+        mb.template keep<SET>(lb);
+        lds_barrier();
+        const int64_t next = k + 2 * kStep < last ? k + 2 * kStep : last;
+        ma.template fetch<SET>(a, next);
+        mb.template fetch<SET>(b, next);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             Fragment<T> fa[4], fb[2];
@@ -375,8 +391,13 @@ __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fa[i], fb[j], acc[i][j]);
         }
-        buffer ^= 1;
+    };
+    int64_t k = k0;
+    for (; k + kStep < k1; k += 2 * kStep) {
+        step(k, std::integral_constant<int, 0>());
+        step(k + kStep, std::integral_constant<int, 1>());
     }
+    if (k < k1) step(k, std::integral_constant<int, 0>());
     __syncthreads();
 }
 __device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 128 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
@@ -385,15 +406,22 @@ __device__ __forceinline__ int acc_col(int j) { return wave_id() % 2 * 64 + j * 
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
+// Workgroups go round the eight XCDs, each with an L2 of its own: tiles next to each other, which share an operand, are
+// given to workgroups of one XCD.
+__device__ __forceinline__ int64_t tile_id() {
+    const int64_t all = gridDim.x, b = blockIdx.x, xcd = b % 8, per = all / 8, more = all % 8;
+    return xcd * per + (xcd < more ? xcd : more) + b / 8;
+}
+
 // ------------------------------------------------------------------------------------------------------- forward
 // A workgroup takes 128 rows and every groups-th tile of 256 vertices; a lane keeps maximum and sum of its two columns.
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x) {
     __shared__ __align__(16) char lds[kLdsBytes];
-    const int64_t n0 = (int64_t)blockIdx.x * kTile;
+    const int64_t id = tile_id(), blocks = a.n_pad / kTile, group = id / blocks, n0 = id % blocks * kTile;
     if (n0 >= (int64_t)a.header->n_live) return;
     float top[2] = {-FLT_MAX, -FLT_MAX}, sum[2] = {};
-    for (int64_t v0 = (int64_t)blockIdx.y * kTileM; v0 < a.V; v0 += (int64_t)a.groups * kTileM) {
+    for (int64_t v0 = group * kTileM; v0 < a.V; v0 += (int64_t)a.groups * kTileM) {
         AccTile acc;
         product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
         if (a.V - v0 < kTileM) {  // behind the last vertex
@@ -439,7 +467,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const float t2 = shared[acc_col(j) * 2], s2 = shared[acc_col(j) * 2 + 1], t = fmaxf(top[j], t2);
-            const int64_t at = (int64_t)blockIdx.y * a.n_pad + n0 + acc_col(j);
+            const int64_t at = group * a.n_pad + n0 + acc_col(j);
             a.part_max[at] = t;
             a.part_sum[at] = sum[j] * exp_of(top[j] - t) + s2 * exp_of(t2 - t);
         }
@@ -490,7 +518,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
                                                          T* __restrict__ probs) {
     __shared__ __align__(16) char lds[kLdsBytes];
     constexpr int kPitch = kTileM + 4;
-    const int64_t n0 = (int64_t)blockIdx.x * kTile, v0 = v_first + (int64_t)blockIdx.y * kTileM;
+    const int64_t id = tile_id(), blocks = a.n_pad / kTile;
+    const int64_t n0 = id % blocks * kTile, m0 = id / blocks * kTileM, v0 = v_first + m0;
     if (n0 >= (int64_t)a.header->n_live) return;
     AccTile acc;
     product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
@@ -517,7 +546,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
                 const int row = acc_row(i, r);
                 const float held = (float)counts[col * kPitch + row];
                 const float p = v0 + row < a.V && c > 0.f ? g * (c * exp_of(acc[i][j][r] - lse) - held) : 0.f;
-                probs[((int64_t)blockIdx.y * kTileM + row) * a.n_pad + n0 + col] = (T)p;
+                probs[(m0 + row) * a.n_pad + n0 + col] = (T)p;
             }
     }
 }
@@ -527,11 +556,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
                                                       T* __restrict__ dw, int64_t dw_stride, float* __restrict__ parts,
-                                                      int64_t part_rows) {
+                                                      int64_t part_rows, int32_t shares) {
     __shared__ __align__(16) char lds[kLdsBytes];
-    const int64_t m0 = (int64_t)blockIdx.x * kTileM, d0 = (int64_t)blockIdx.y * kTileN;
+    // the tiles of one share, and of one tile of vertices, next to each other
+    const int64_t id = tile_id(), d_tiles = (a.dp + kTileN - 1) / kTileN, v_tiles = gridDim.x / (d_tiles * shares);
+    const int64_t d0 = id % d_tiles * kTileN, m0 = id / d_tiles % v_tiles * kTileM, share = id / (d_tiles * v_tiles);
     const int64_t steps = ((int64_t)a.header->n_live + Kind<T>::kStep - 1) / Kind<T>::kStep;
-    const int64_t k0 = steps * blockIdx.z / gridDim.z * Kind<T>::kStep, k1 = steps * (blockIdx.z + 1) / gridDim.z * Kind<T>::kStep;
+    const int64_t k0 = steps * share / shares * Kind<T>::kStep, k1 = steps * (share + 1) / shares * Kind<T>::kStep;
     AccTile acc;
     product<T, false, true>(probs, x, m0, d0, k0, k1, lds, acc);
     const float back = 1.f / a.header->scale;
@@ -545,10 +576,10 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
             for (int r = 0; r < 16; ++r) {
                 const int64_t m = m0 + acc_row(i, r);
                 if (v_first + m >= a.V) continue;
-                if (gridDim.z == 1)
+                if (shares == 1)
                     dw[(v_first + m) * dw_stride + e] = (T)(acc[i][j][r] * back);
                 else
-                    parts[((int64_t)blockIdx.z * part_rows + m) * a.dp + e] = acc[i][j][r];
+                    parts[(share * part_rows + m) * a.dp + e] = acc[i][j][r];
             }
     }
 }
@@ -566,34 +597,35 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const flo
         }
 }
 
-// dx of 256 numbers of 128 rows, summed over a share of the piece's vertices.
+// dx of 256 rows and 128 numbers, summed over a share of the piece's vertices.
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
                                                       int64_t v_share, int64_t v_end, int first_piece,
                                                       float* __restrict__ parts) {
     __shared__ __align__(16) char lds[kLdsBytes];
-    const int64_t n0 = (int64_t)blockIdx.x * kTile, d0 = (int64_t)blockIdx.y * kTileM;
+    // the tiles of one share, and of one tile of rows, next to each other
+    const int64_t id = tile_id(), d_tiles = (a.dp + kTileN - 1) / kTileN, n_tiles = a.n_pad / kTileM;
+    const int64_t d0 = id % d_tiles * kTileN, n0 = id / d_tiles % n_tiles * kTileM, share = id / (d_tiles * n_tiles);
     if (n0 >= (int64_t)a.header->n_live) return;
-    const int64_t k0 = (int64_t)blockIdx.z * v_share;
+    const int64_t k0 = share * v_share;
     const int64_t k1 = k0 + v_share < v_end ? k0 + v_share : v_end;
     Operand<T> piece = w;
     piece.base += v_first * w.stride;
     piece.rows -= v_first;
     AccTile acc;
-    product<T, true, true>(piece, probs, d0, n0, k0, k1, lds, acc);
-    typedef float Float4 __attribute__((ext_vector_type(4)));
+    product<T, true, true>(probs, piece, n0, d0, k0, k1, lds, acc);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+        const int64_t e = d0 + acc_col(j);
+        if (e >= a.dp) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int64_t e = d0 + acc_row(i, r);
-                if (e >= a.dp) continue;
-                Float4* at = reinterpret_cast<Float4*>(parts + ((int64_t)blockIdx.z * a.n_pad + n0 + acc_col(j)) * a.dp + e);
-                const Float4 v = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-                *at = first_piece ? v : *at + v;
+            for (int r = 0; r < 16; ++r) {
+                float* at = parts + (share * a.n_pad + n0 + acc_row(i, r)) * a.dp + e;
+                *at = first_piece ? acc[i][j][r] : *at + acc[i][j][r];
             }
+    }
 }
 
 template <typename T>
@@ -635,23 +667,24 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     p.sweep = dtype != ND_F32 && sweep_width(d) > 0;
     p.dp = p.sweep ? sweep_width(d) : (int32_t)((d + step - 1) / step * step);
     p.blocks = n > 0 ? (n + kTile - 1) / kTile : 1;  // without rows: the header is written all the same
-    p.n_pad = p.blocks * kTile;
+    p.n_pad = (p.blocks * kTile + kTileM - 1) / kTileM * kTileM;
     const int64_t v_tiles = (V + kTileM - 1) / kTileM;
-    // enough workgroups to fill the chip several times over
-    const int64_t groups = (1024 + p.blocks - 1) / p.blocks;
+    // two workgroups per compute unit at a time, and all of them with about as many tiles
+    const int64_t n_tiles = p.n_pad / kTile, groups = n_tiles < 512 ? 512 / n_tiles : 1;
     p.groups = (int32_t)(groups < v_tiles ? groups : v_tiles);
     int64_t piece_tiles = (int64_t)(kPieceBytes / (size_t)(p.n_pad * kTileM * b));
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > 32768) piece_tiles = 32768;
     if (piece_tiles > v_tiles) piece_tiles = v_tiles;
     p.piece = piece_tiles * kTileM;
-    // the summed dimension is shared out where there are fewer tiles than two per compute unit
+    // the summed dimension is shared out where there are fewer tiles than two per compute unit; one more than that would
+    // take as long as twice as many
     auto shares = [](int64_t tiles, int64_t most) {
-        int64_t s = (512 + tiles - 1) / tiles;
+        int64_t s = tiles < 512 ? 512 / tiles : 1;
         s = s < 16 ? s : 16;
         return (int32_t)(s < most ? s : most);
     };
-    p.shares = shares(p.blocks * ((p.dp + kTileM - 1) / kTileM), piece_tiles);
+    p.shares = shares(p.n_pad / kTileM * ((p.dp + kTileN - 1) / kTileN), piece_tiles);
     p.dw_shares = shares(piece_tiles * ((p.dp + kTileN - 1) / kTileN), p.blocks);
     size_t o = sizeof(LossHeader);
     auto take = [&](size_t bytes) {
@@ -830,27 +863,28 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         }
     const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
     if (c.n > 0) {
-        hipLaunchKernelGGL(stats_kernel<T>, dim3(blocks, (unsigned)p.groups), dim3(kThreads), 0, stream, a, ow, ox);
+        hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(p.n_pad / kTile * p.groups)), dim3(kThreads), 0, stream, a, ow, ox);
         hipLaunchKernelGGL(loss_kernel<T>, wave_per(c.n), dim3(kThreads), 0, stream, a, rows, w, w_stride);
     }
     if (c.grad) {
         T* probs = (T*)(ws + p.o_probs);
         float* parts = (float*)(ws + p.o_parts);
         float* dw_parts = (float*)(ws + p.o_dw_parts);
+        const int64_t d_tiles = (p.dp + kTileN - 1) / kTileN;
         for (int64_t v = 0; v < c.V; v += p.piece) {
             const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTileM - 1) / kTileM;
             const Operand<T> op{probs, p.n_pad, tiles * kTileM, (int32_t)p.n_pad};
             if (c.n > 0)
-                hipLaunchKernelGGL(probs_kernel<T>, dim3(blocks, (unsigned)tiles), dim3(kThreads), 0, stream, a, ow, ox, v, probs);
+                hipLaunchKernelGGL(probs_kernel<T>, dim3((unsigned)(p.n_pad / kTile * tiles)), dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)
-                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)tiles, (unsigned)((p.dp + kTileN - 1) / kTileN), (unsigned)p.dw_shares),
-                                   dim3(kThreads), 0, stream, a, op, ox, v, (T*)c.dw, c.dw_stride, dw_parts, p.piece);
+                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)(tiles * d_tiles * p.dw_shares)), dim3(kThreads), 0, stream, a, op, ox, v,
+                                   (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares);
             if (c.dw && p.dw_shares > 1)
                 hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
                                    here, (T*)c.dw, c.dw_stride);
             if (c.dx && c.n > 0) {
                 const int64_t share = (tiles + p.shares - 1) / p.shares * kTileM;
-                hipLaunchKernelGGL(dx_kernel<T>, dim3(blocks, (unsigned)((p.dp + kTileM - 1) / kTileM), (unsigned)p.shares), dim3(kThreads), 0, stream, a, op, ow,
+                hipLaunchKernelGGL(dx_kernel<T>, dim3((unsigned)(p.n_pad / kTileM * d_tiles * p.shares)), dim3(kThreads), 0, stream, a, op, ow,
                                    v, share, tiles * kTileM, (int)(v == 0), parts);
             }
         }
