@@ -7,7 +7,6 @@
 namespace nd {
 
 constexpr int kSweepHeld = 256;     // held rows of a tile
-constexpr int kSweepUnit = 64;      // passing rows at a time
 constexpr int kSweepGroups = 256;   // workgroups: one per compute unit
 constexpr int kSweepLeast = 4;      // units that a workgroup takes at least
 
@@ -17,14 +16,17 @@ enum SweepMode {
     kSweepDw = 2,    // w held, x passes: sums of x's rows weighted with g c p, less the sums over labels
 };
 
+// Passing rows at a time: as many as make 1,024 cycles of matrix instructions per wavefront between two barriers.
+constexpr int sweep_unit(int mode, int d) { return mode != kSweepLse && d > 128 ? 32 : 64; }
+
 // How the work, tiles of held rows x units of passing rows, is dealt out: workgroup g takes the units
 // [g total / groups, (g + 1) total / groups) of all tiles in a row, so that every one has as many, whatever the number of
 // tiles; what it holds of a tile is a segment.
 struct SweepDeal {
     int64_t tiles, units, total, groups;
-    __host__ __device__ SweepDeal(int64_t held, int held_tile, int64_t passing) {
+    __host__ __device__ SweepDeal(int64_t held, int held_tile, int64_t passing, int unit) {
         tiles = (held + held_tile - 1) / held_tile;
-        units = (passing + kSweepUnit - 1) / kSweepUnit;
+        units = (passing + unit - 1) / unit;
         total = tiles * units;
         groups = total / kSweepLeast;
         if (groups > kSweepGroups) groups = kSweepGroups;

@@ -1,6 +1,5 @@
 #include "nd_sweep.h"
 
-#include <cfloat>
 #include <type_traits>
 
 #include "nd_wave.h"
@@ -18,6 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLowest = -1e38f;  // below every maximum, and finite times log2 e
 
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef float Float4 __attribute__((ext_vector_type(4)));
@@ -46,9 +46,10 @@ struct Shape {
     static constexpr int kRing = kAhead ? 4 : 2;       // units in LDS
     static constexpr int kSteps = D / 16;              // instructions along a row
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
-    static constexpr int kUnitBytes = kSweepUnit * D * 2;
+    static constexpr int kUnit = sweep_unit(MODE, D);
+    static constexpr int kUnitBytes = kUnit * D * 2;
     static constexpr int kLoads = kUnitBytes / (kThreads * 16);  // pieces that a lane moves per unit
-    static constexpr int kFactorBytes = MODE == kSweepDw ? 2 * kSweepUnit * 4 : 0;  // what the passing rows weigh
+    static constexpr int kFactorBytes = MODE == kSweepDw ? 2 * kUnit * 4 : 0;  // what the passing rows weigh
     static constexpr int kLds = kRing * (kUnitBytes + kFactorBytes);
 };
 
@@ -82,7 +83,7 @@ template <typename T, int D, int MODE>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) void sweep_kernel(LossArgs a, SweepArgs s) {
     using Sh = Shape<MODE, D>;
     using V8 = typename Eight<T>::V;
-    constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing;
+    constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing, UNIT = Sh::kUnit;
     constexpr bool kSums = MODE != kSweepLse, kOnline = MODE != kSweepDw, kAhead = Sh::kAhead;
     // fp16 ends at 2^-24: exponentials are taken times 2^8 and may outgrow the maximum that they are relative to by 2^6
     constexpr float kRaise = std::is_same<T, f16_t>::value ? 8.f : 0.f;
@@ -92,24 +93,27 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
     const int64_t live = a.header->n_live;
     const int64_t held_rows = MODE == kSweepDw ? a.V : live, passing_rows = MODE == kSweepDw ? live : a.V;
     if (held_rows == 0 || passing_rows == 0) return;
-    const SweepDeal deal(held_rows, HELD, passing_rows);
+    const SweepDeal deal(held_rows, HELD, passing_rows, UNIT);
     if ((int64_t)blockIdx.x >= deal.groups) return;
     const T* held = (const T*)s.held;
     const T* passing = (const T*)s.passing;
     float* factors = (float*)(lds + RING * Sh::kUnitBytes);                    // [unit][lse log2 e, g c][passing row]
     const float scale = MODE == kSweepDw ? a.header->scale : 1.f;
 
-    // where a lane reads in a unit: pieces of a row (a block's 32 rows), and four rows of a column's 8 bytes (16 rows); what
-    // the kernel adds to them is known when it is compiled
+    // Where a lane reads in a unit: piece 2 k + half of one of a block's 32 rows, and column_at[e][j]: of the rows 8 e + 4
+    // half to + 3 of a block of 16, eight bytes in columns 32 j on.  What the kernel adds to them is known when it is
+    // compiled.  k and e, j only turn bits over (see place), so that short of registers they are made from one place each.
     typedef LdsOf<char> LdsChar;
     LdsChar* unit_lds = (LdsChar*)lds;
-    int32_t score_at[STEPS < 8 ? STEPS : 8], column_at[2][D / 32 < 4 ? D / 32 : 4];
+    constexpr bool kTight = !kAhead && kSums;
+    constexpr int kScoreAt = kTight ? 1 : STEPS < 8 ? STEPS : 8, kColumnAt = kTight ? 1 : D / 32 < 4 ? D / 32 : 4;
+    int32_t score_at[kScoreAt], column_at[kTight ? 1 : 2][kColumnAt];
 #pragma unroll
-    for (int k = 0; k < (STEPS < 8 ? STEPS : 8); ++k) score_at[k] = place<D>(col, k * 2 + half);
+    for (int k = 0; k < kScoreAt; ++k) score_at[k] = place<D>(col, k * 2 + half);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int e = 0; e < (kTight ? 1 : 2); ++e)
 #pragma unroll
-        for (int j = 0; j < (D / 32 < 4 ? D / 32 : 4); ++j) {
+        for (int j = 0; j < kColumnAt; ++j) {
             const int sub = lane & 15, at = j * 32 + ((lane >> 4) & 1) * 16 + (sub & 3) * 4;
             column_at[e][j] = place<D>(e * 8 + half * 4 + (sub >> 2), at / 8) + (at & 4) * 2;
         }
@@ -130,12 +134,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         Word4 ahead[Sh::kLoads];
         float factor_ahead[3];
         auto load = [&](int32_t u) {
-            // gathered rows are padded with zeros to whole units, but no further
             // No branches: what is loaded must not be waited for here.  Rows behind the last one are the last one again;
             // gathered rows are padded with zeros to whole units, but no further.
-            const int64_t r0 = (int64_t)u * kSweepUnit, left = (MODE == kSweepDw ? deal.units * kSweepUnit : passing_rows) - r0;
+            const int64_t r0 = (int64_t)u * UNIT, left = (MODE == kSweepDw ? deal.units * UNIT : passing_rows) - r0;
             const int64_t from_row = left > 0 ? r0 : 0;
-            const uint32_t last = left > kSweepUnit ? kSweepUnit - 1 : left > 0 ? (uint32_t)left - 1u : 0u;
+            const uint32_t last = left > UNIT ? UNIT - 1 : left > 0 ? (uint32_t)left - 1u : 0u;
             const char* from = (const char*)(passing + from_row * s.passing_stride);
             const uint32_t row_bytes = (uint32_t)s.passing_stride * 2u;
 #pragma unroll
@@ -144,7 +147,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                 ahead[i] = *reinterpret_cast<const Word4*>(from + ((r < last ? r : last) * row_bytes + e % Sh::kPieces * 16u));
             }
             if (MODE == kSweepDw) {
-                const int64_t p = from_row + (threadIdx.x & (kSweepUnit - 1));
+                const int64_t p = from_row + (threadIdx.x & (UNIT - 1));
                 factor_ahead[0] = a.place_lse[p];
                 factor_ahead[1] = a.count[p];
                 factor_ahead[2] = a.weight[p];
@@ -156,11 +159,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                 const int e = i * THREADS + (int)threadIdx.x;
                 *reinterpret_cast<Word4*>(lds + slot * Sh::kUnitBytes + place<D>(e / Sh::kPieces, e % Sh::kPieces)) = ahead[i];
             }
-            if (MODE == kSweepDw && threadIdx.x < kSweepUnit) {
+            if (MODE == kSweepDw && threadIdx.x < UNIT) {
                 // behind the segment's last unit nothing weighs
-                float* f = factors + slot * 2 * kSweepUnit + threadIdx.x;
+                float* f = factors + slot * 2 * UNIT + threadIdx.x;
                 f[0] = u < u1 ? factor_ahead[0] * kLog2e : INFINITY;
-                f[kSweepUnit] = u < u1 ? factor_ahead[1] * factor_ahead[2] * scale : 0.f;
+                f[UNIT] = u < u1 ? factor_ahead[1] * factor_ahead[2] * scale : 0.f;
             }
         };
 
@@ -176,7 +179,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         Acc sums[D / 32];
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) sums[j] = Acc{};
-        float top = -FLT_MAX, top2 = 0.f, total = 0.f;  // maximum, the same in the exponent of 2, sum
+        float top = kLowest, top2 = kLowest * kLog2e, total = 0.f;  // maximum, the same in the exponent of 2, sum
 
         lds_barrier();  // the segment before has read its units
         if (kAhead)  // what the sums read in front of the first block
@@ -193,8 +196,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
 
         // ---- operands from LDS: a piece of 32 passing rows for the scores; 16 passing rows down 32 columns for the sums
         auto row_piece = [&](int slot, int b, int k) {
-            return *reinterpret_cast<const LdsOf<V8>*>(unit_lds + score_at[k & 7] +
-                                                       (slot * Sh::kUnitBytes + b * 32 * D * 2 + (k >> 3) * 256));
+            const int32_t at = kTight ? score_at[0] ^ ((k & 7) * 32) : score_at[kTight ? 0 : k & 7];
+            return *reinterpret_cast<const LdsOf<V8>*>(unit_lds + at + (slot * Sh::kUnitBytes + b * 32 * D * 2 + (k >> 3) * 256));
         };
         auto column_piece = [&](int slot, int b, int i) {
             const int t = i / (D / 32), j = i % (D / 32);
@@ -203,9 +206,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                 Short4 q[2];
             } p;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+            for (int e = 0; e < 2; ++e) {
+                const int32_t at = kTight ? (column_at[0][0] ^ ((j & 3) * 64 + e * 32)) + e * 8 * D * 2 : column_at[kTight ? 0 : e][kTight ? 0 : j & 3];
                 p.q[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsOf<Short4>*>(
-                    unit_lds + column_at[e][j & 3] + (slot * Sh::kUnitBytes + (b * 32 + t * 16) * D * 2 + (j >> 2) * 256)));
+                    unit_lds + at + (slot * Sh::kUnitBytes + (b * 32 + t * 16) * D * 2 + (j >> 2) * 256)));
+            }
             return p.v;
         };
         // ---- scores of block b of the unit in `slot`
@@ -248,14 +253,14 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         const int32_t masked = u1 == (int32_t)deal.units ? u1 - 1 : u1;
         auto mask = [&](Acc& now, int32_t u, int b) {
             if (u < masked) return;
-            const int64_t left = passing_rows - (int64_t)u * kSweepUnit;
-            const int32_t rows_left = u >= u1 ? 0 : left < kSweepUnit ? (int32_t)left : kSweepUnit;
+            const int64_t left = passing_rows - (int64_t)u * UNIT;
+            const int32_t rows_left = u >= u1 ? 0 : left < UNIT ? (int32_t)left : UNIT;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (half * 4 >= rows_left - (b * 32 + 8 * (r / 4) + r % 4)) now[r] = -INFINITY;
         };
-        // ---- weights of a block from its scores, 16 / STEPS' share i of them
-        constexpr int kShare = 16 / (STEPS < 16 ? STEPS : 16);
+        // ---- weights of a block from its scores, share i of them
+        constexpr int kShare = kAhead ? 16 / STEPS : 4;
         float part;      // the block's sum
         uint32_t most;   // and its largest weight, as the bits of a number that is not negative
         auto weights_of = [&](const Acc& now, V8 (&weight)[2], int i) {
@@ -294,9 +299,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         Few lse_ahead, gc_ahead;
         auto load_factors = [&](int slot, int b, int i) {
             const int r = i * kShare;
-            const int at = (slot * 2 * kSweepUnit + b * 32 + 8 * (r / 4) + r % 4) * 4;
+            const int at = (slot * 2 * UNIT + b * 32 + 8 * (r / 4) + r % 4) * 4;
             lse_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at);
-            gc_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at + kSweepUnit * 4);
+            gc_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at + UNIT * 4);
         };
         auto dw_weights_of = [&](const Acc& now, V8 (&weight)[2], int slot, int b, int i) {
             const Few lse = lse_ahead, gc = gc_ahead;
@@ -321,14 +326,16 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
             constexpr int next = (slot + 1) & (RING - 1), previous = (slot + RING - 1) & (RING - 1);
             keep(u + (kAhead ? 2 : 1), (slot + (kAhead ? 2 : 1)) & (RING - 1));
             load(u + (kAhead ? 3 : 2));
+            if (kTight) asm volatile("" : "+v"(score_at[0]), "+v"(column_at[0][0]));  // not all made in front of the loop
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < UNIT / 32; ++b) {
                 // Ahead: this block's weights, while the next block's scores and the sums over the block before are made
                 // (in front of the first block: weights of zero, of a unit that starts as zeros).
                 Acc& now = score[kAhead ? b : 0];
                 V8(&mine)[2] = weight[kAhead ? b : 0];
                 const int next_slot = b == 0 ? slot : next, before_slot = b == 0 ? previous : slot;
                 if (!kAhead) scores(now, slot, b);
+                if (kTight) __builtin_amdgcn_sched_barrier(0);  // what the steps read of LDS takes turns in the registers left
                 if (kOnline) {
                     mask(now, u, b);
                     if (kAhead)
@@ -348,6 +355,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
                         for (int i = 0; i < 16 / kShare; ++i) dw_weights_of(now, mine, slot, b, i);
                 }
                 if (kSums) asm volatile("" : "+v"(mine[0]), "+v"(mine[1]));  // made here, not where they are used
+                if (kTight) __builtin_amdgcn_sched_barrier(0);
                 if (!kAhead && kSums) add_rows(mine, slot, b);
             }
             lds_barrier();
@@ -422,7 +430,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepParts parts, T* __restrict__ dw, int64_t dw_stride) {
     constexpr int HELD = kSweepHeld, kRows = 32, kQuads = D / 4;
     const int64_t live = a.header->n_live;
-    const SweepDeal deal(a.V, HELD, live);
+    const SweepDeal deal(a.V, HELD, live, sweep_unit(kSweepDw, D));
     const float back = 1.f / a.header->scale;
     for (int64_t v0 = (int64_t)blockIdx.x * kRows; v0 < a.V; v0 += (int64_t)gridDim.x * kRows) {
         int64_t x0 = 0, g0 = 0, g1 = -1;
@@ -467,7 +475,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
     constexpr int PER = D / 64;     // numbers of a lane
     constexpr int kAtOnce = 5;      // labels' rows under way
     const int64_t live = a.header->n_live;
-    const SweepDeal deal(live, HELD, a.V);
+    const SweepDeal deal(live, HELD, a.V, sweep_unit(MODE, D));
     const int e0 = lane_id() * PER;
     for (int64_t p0 = (int64_t)blockIdx.x * kFinishRows; p0 < live; p0 += (int64_t)gridDim.x * kFinishRows) {
         const int64_t tile = p0 / HELD, x0 = tile * deal.units;
@@ -476,7 +484,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
             const int64_t in_tile = p % HELD, row = a.row_of[p];
             const int32_t my_label = lane_id() < a.k ? a.labels_of[p * a.k + lane_id()] : -1;
             const Piece<T, PER> x = load_piece<T, PER>(rows + p * D + e0);
-            float top = -FLT_MAX, sum = 0.f;
+            float top = kLowest, sum = 0.f;
             for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
                 const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile], t = fmaxf(top, t2);
                 sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
