@@ -6,8 +6,6 @@
 
 namespace nd {
 
-constexpr int kSweepHeld = 256;     // held rows of a tile
-constexpr int kSweepGroups = 256;   // workgroups: one per compute unit
 constexpr int kSweepLeast = 4;      // units that a workgroup takes at least
 
 enum SweepMode {
@@ -16,20 +14,33 @@ enum SweepMode {
     kSweepDw = 2,    // w held, x passes: sums of x's rows weighted with g c p, less the sums over labels
 };
 
-// Passing rows at a time: as many as make 1,024 cycles of matrix instructions per wavefront between two barriers.
-constexpr int sweep_unit(int mode, int d) { return mode != kSweepLse && d > 128 ? 32 : 64; }
+// What a workgroup of the sweep in a mode over rows of d numbers is: wavefronts, 32 held rows each; passing rows at a time;
+// how many there are, all of them at work at once.
+struct SweepShape {
+    int waves, unit, per_cu;
+    constexpr int held() const { return 32 * waves; }
+    constexpr int groups() const { return 256 * per_cu; }
+};
+constexpr SweepShape sweep_shape(int mode, int d) {
+    // Registers leave room for two workgroups where few sums are kept: 14,250 x 57,000 x 128 forward 230 us, 248 with one;
+    // over rows of 64 numbers 159 and 187, with dx (8,192 rows) 138 and 152.
+    if (mode == kSweepLse) return d > 128 ? SweepShape{8, 64, 1} : SweepShape{8, 64, 2};
+    if (mode == kSweepDx && d <= 64) return SweepShape{8, 64, 2};
+    // two of these blocks of 32 rows are a unit of the others
+    return d > 128 ? SweepShape{8, 32, 1} : SweepShape{8, 64, 1};
+}
 
 // How the work, tiles of held rows x units of passing rows, is dealt out: workgroup g takes the units
 // [g total / groups, (g + 1) total / groups) of all tiles in a row, so that every one has as many, whatever the number of
 // tiles; what it holds of a tile is a segment.
 struct SweepDeal {
     int64_t tiles, units, total, groups;
-    __host__ __device__ SweepDeal(int64_t held, int held_tile, int64_t passing, int unit) {
-        tiles = (held + held_tile - 1) / held_tile;
-        units = (passing + unit - 1) / unit;
+    __host__ __device__ SweepDeal(int64_t held, int64_t passing, SweepShape shape) {
+        tiles = (held + shape.held() - 1) / shape.held();
+        units = (passing + shape.unit - 1) / shape.unit;
         total = tiles * units;
         groups = total / kSweepLeast;
-        if (groups > kSweepGroups) groups = kSweepGroups;
+        if (groups > shape.groups()) groups = shape.groups();
         if (groups < 1) groups = 1;
     }
     __host__ __device__ int64_t first(int64_t g) const { return g * total / groups; }
@@ -81,7 +92,7 @@ struct SweepParts {
     const float* label_sums;
 };
 int sweep_width(int32_t d);                   // numbers in a padded row, 0: rows are too long
-int64_t sweep_segments(int mode, int64_t held);
+int64_t sweep_rows(int mode, int64_t held, int32_t dp);  // held rows of all segments
 template <typename T>
 int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stride, const SweepParts& parts, T* dw,
           int64_t dw_stride, hipStream_t stream);

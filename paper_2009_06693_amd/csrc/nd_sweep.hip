@@ -38,18 +38,21 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 
 template <int MODE, int D>
 struct Shape {
-    static constexpr int kThreads = 512;               // two wavefronts per SIMD: one multiplies while the other takes exponentials
-    static constexpr int kHeld = kSweepHeld;           // 32 held rows per wavefront
+    static constexpr SweepShape kShape = sweep_shape(MODE, D);
+    static constexpr int kThreads = 64 * kShape.waves;
+    static constexpr int kWaves = kShape.waves * kShape.per_cu / 4;  // of a SIMD
+    static constexpr int kHeld = kShape.held();
     // A block's scores are made while the block before is still being worked on, where there are registers for both
-    // (of 256: D / 8 for the held rows, D / 2 for the sums, 16 + 8 per block under way).
-    static constexpr bool kAhead = D <= 128;
+    // (of 256: D / 8 for the held rows, D / 2 for the sums, 16 + 8 per block under way) and no second workgroup to fill in.
+    static constexpr bool kAhead = MODE != kSweepLse && D <= 128 && kShape.per_cu == 1;
     static constexpr int kRing = kAhead ? 4 : 2;       // units in LDS
     static constexpr int kSteps = D / 16;              // instructions along a row
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
-    static constexpr int kUnit = sweep_unit(MODE, D);
+    static constexpr int kUnit = kShape.unit;
     static constexpr int kUnitBytes = kUnit * D * 2;
     static constexpr int kLoads = kUnitBytes / (kThreads * 16);  // pieces that a lane moves per unit
-    static constexpr int kFactorBytes = MODE == kSweepDw ? 2 * kUnit * 4 : 0;  // what the passing rows weigh
+    // kSweepDw: what the passing rows weigh, and signs of two rows in a word
+    static constexpr int kFactorBytes = MODE == kSweepDw ? kUnit * 4 + kUnit * 2 : 0;
     static constexpr int kLds = kRing * (kUnitBytes + kFactorBytes);
 };
 
@@ -80,24 +83,24 @@ struct SweepArgs {
 };
 
 template <typename T, int D, int MODE>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) void sweep_kernel(LossArgs a, SweepArgs s) {
+__global__ __attribute__((amdgpu_waves_per_eu(Shape<MODE, D>::kWaves, Shape<MODE, D>::kWaves))) __launch_bounds__((Shape<MODE, D>::kThreads)) void sweep_kernel(LossArgs a, SweepArgs s) {
     using Sh = Shape<MODE, D>;
     using V8 = typename Eight<T>::V;
     constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing, UNIT = Sh::kUnit;
     constexpr bool kSums = MODE != kSweepLse, kOnline = MODE != kSweepDw, kAhead = Sh::kAhead;
     // fp16 ends at 2^-24: exponentials are taken times 2^8 and may outgrow the maximum that they are relative to by 2^6
     constexpr float kRaise = std::is_same<T, f16_t>::value ? 8.f : 0.f;
-    const uint32_t kMost = __float_as_uint(std::is_same<T, f16_t>::value ? 16384.f : 64.f);  // 2^6 times that
+    constexpr float kMost = std::is_same<T, f16_t>::value ? 16384.f : 64.f;  // 2^6 times that
     extern __shared__ __align__(16) char lds[];
     const int lane = lane_id(), wave = (int)wave_uniform((uint32_t)wave_id()), half = lane >> 5, col = lane & 31;
     const int64_t live = a.header->n_live;
     const int64_t held_rows = MODE == kSweepDw ? a.V : live, passing_rows = MODE == kSweepDw ? live : a.V;
     if (held_rows == 0 || passing_rows == 0) return;
-    const SweepDeal deal(held_rows, HELD, passing_rows, UNIT);
+    const SweepDeal deal(held_rows, passing_rows, Sh::kShape);
     if ((int64_t)blockIdx.x >= deal.groups) return;
     const T* held = (const T*)s.held;
     const T* passing = (const T*)s.passing;
-    float* factors = (float*)(lds + RING * Sh::kUnitBytes);                    // [unit][lse log2 e, g c][passing row]
+    char* factors = lds + RING * Sh::kUnitBytes;  // [unit]: exponents of 2, a float per passing row; signs, 16 bits per row
     const float scale = MODE == kSweepDw ? a.header->scale : 1.f;
 
     // Where a lane reads in a unit: piece 2 k + half of one of a block's 32 rows, and column_at[e][j]: of the rows 8 e + 4
@@ -105,7 +108,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
     // compiled.  k and e, j only turn bits over (see place), so that short of registers they are made from one place each.
     typedef LdsOf<char> LdsChar;
     LdsChar* unit_lds = (LdsChar*)lds;
-    constexpr bool kTight = !kAhead && kSums;
+    constexpr bool kTight = D > 128 && kSums;
     constexpr int kScoreAt = kTight ? 1 : STEPS < 8 ? STEPS : 8, kColumnAt = kTight ? 1 : D / 32 < 4 ? D / 32 : 4;
     int32_t score_at[kScoreAt], column_at[kTight ? 1 : 2][kColumnAt];
 #pragma unroll
@@ -118,9 +121,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
             column_at[e][j] = place<D>(e * 8 + half * 4 + (sub >> 2), at / 8) + (at & 4) * 2;
         }
 
-    // behind what an instruction's offset reaches from the front of LDS: the lane's own place, kept in a register
-    LdsChar* factor_lds = unit_lds + RING * Sh::kUnitBytes + half * 16;
-    if (MODE == kSweepDw) asm volatile("" : "+v"(factor_lds));
+    // behind what an instruction's offset reaches from the front of LDS: the lane's own places, kept in registers
+    LdsChar *factor_lds = unit_lds + RING * Sh::kUnitBytes + half * 16, *sign_lds = unit_lds + RING * Sh::kUnitBytes + UNIT * 4 + half * 8;
+    if (MODE == kSweepDw) asm volatile("" : "+v"(factor_lds), "+v"(sign_lds));
 
     const int64_t end = deal.first((int64_t)blockIdx.x + 1);
     for (int64_t x = deal.first(blockIdx.x); x < end;) {
@@ -161,9 +164,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
             }
             if (MODE == kSweepDw && threadIdx.x < UNIT) {
                 // behind the segment's last unit nothing weighs
-                float* f = factors + slot * 2 * UNIT + threadIdx.x;
-                f[0] = u < u1 ? factor_ahead[0] * kLog2e : INFINITY;
-                f[UNIT] = u < u1 ? factor_ahead[1] * factor_ahead[2] * scale : 0.f;
+                // g c exp(s - lse) = sign(g c) exp2(s log2 e - (lse log2 e - log2 |g c|))
+                const float gc = factor_ahead[1] * factor_ahead[2] * scale;
+                char* f = factors + slot * Sh::kFactorBytes;
+                reinterpret_cast<float*>(f)[threadIdx.x] = u < u1 ? factor_ahead[0] * kLog2e - log2f(fabsf(gc)) : INFINITY;
+                reinterpret_cast<uint16_t*>(f + UNIT * 4)[threadIdx.x] = gc < 0.f ? 0x8000 : 0;
             }
         };
 
@@ -261,23 +266,20 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         };
         // ---- weights of a block from its scores, share i of them
         constexpr int kShare = kAhead ? 16 / STEPS : 4;
-        float part;      // the block's sum
-        uint32_t most;   // and its largest weight, as the bits of a number that is not negative
+        float part;  // the block's sum
         auto weights_of = [&](const Acc& now, V8 (&weight)[2], int i) {
 #pragma unroll
             for (int r = i * kShare; r < (i + 1) * kShare; ++r) {
                 float p = exp2_of(fmaf(now[r], kLog2e, -top2));
                 asm volatile("" : "+v"(p));  // made in this share
-                const uint32_t bits = __float_as_uint(p);
                 part = r == 0 ? p : part + p;
-                most = r == 0 ? bits : (most > bits ? most : bits);
                 if (kSums) weight[r / 8][r % 8] = (T)p;
             }
         };
-        // ---- The maximum moves only where a weight has outgrown it, and for a segment's first block: seldom.  The sums do not
-        // hold the block yet.
+        // ---- The maximum moves only where a weight may have outgrown it, as a lane's sum of 16 tells without a comparison each,
+        // and for a segment's first block: seldom.  The sums do not hold the block yet.
         auto settle = [&](const Acc& now, V8 (&weight)[2], bool first) {
-            if (first || __ballot(most > kMost)) {
+            if (first || __ballot(!(part <= kMost))) {
                 float t = now[0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) t = fmaxf(t, now[r]);
@@ -296,22 +298,27 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
         };
         // factors of a share's rows: read a share ahead
         typedef float Few __attribute__((ext_vector_type(kShare)));
-        Few lse_ahead, gc_ahead;
+        typedef uint32_t Signs __attribute__((ext_vector_type(kShare / 2)));
+        Few lse_ahead;
+        Signs signs_ahead;
         auto load_factors = [&](int slot, int b, int i) {
-            const int r = i * kShare;
-            const int at = (slot * 2 * UNIT + b * 32 + 8 * (r / 4) + r % 4) * 4;
-            lse_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at);
-            gc_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + at + UNIT * 4);
+            const int r = i * kShare, row = b * 32 + 8 * (r / 4) + r % 4;
+            lse_ahead = *reinterpret_cast<const LdsOf<Few>*>(factor_lds + slot * Sh::kFactorBytes + row * 4);
+            signs_ahead = *reinterpret_cast<const LdsOf<Signs>*>(sign_lds + slot * Sh::kFactorBytes + row * 2);
         };
         auto dw_weights_of = [&](const Acc& now, V8 (&weight)[2], int slot, int b, int i) {
-            const Few lse = lse_ahead, gc = gc_ahead;
+            const Few lse = lse_ahead;
+            const Signs signs = signs_ahead;
             if (i + 1 < 16 / kShare) load_factors(slot, b, i + 1);
 #pragma unroll
-            for (int e = 0; e < kShare; ++e) {
+            for (int e = 0; e < kShare; e += 2) {
+                typedef T V2 __attribute__((ext_vector_type(2)));
                 const int r = i * kShare + e;
-                float p = gc[e] * exp2_of(fmaf(now[r], kLog2e, -lse[e]));
-                asm volatile("" : "+v"(p));
-                weight[r / 8][r % 8] = (T)p;
+                float p0 = exp2_of(fmaf(now[r], kLog2e, -lse[e])), p1 = exp2_of(fmaf(now[r + 1], kLog2e, -lse[e + 1]));
+                asm volatile("" : "+v"(p0), "+v"(p1));
+                const V2 p = __builtin_bit_cast(V2, __builtin_bit_cast(uint32_t, V2{(T)p0, (T)p1}) ^ signs[e / 2]);
+                weight[r / 8][r % 8] = p[0];
+                weight[r / 8][r % 8 + 1] = p[1];
             }
         };
 
@@ -428,9 +435,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(512) voi
 // rows of a tile, its lanes four numbers each.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepParts parts, T* __restrict__ dw, int64_t dw_stride) {
-    constexpr int HELD = kSweepHeld, kRows = 32, kQuads = D / 4;
+    constexpr int HELD = sweep_shape(kSweepDw, D).held(), kRows = 32, kQuads = D / 4;
     const int64_t live = a.header->n_live;
-    const SweepDeal deal(a.V, HELD, live, sweep_unit(kSweepDw, D));
+    const SweepDeal deal(a.V, live, sweep_shape(kSweepDw, D));
     const float back = 1.f / a.header->scale;
     for (int64_t v0 = (int64_t)blockIdx.x * kRows; v0 < a.V; v0 += (int64_t)gridDim.x * kRows) {
         int64_t x0 = 0, g0 = 0, g1 = -1;
@@ -471,11 +478,11 @@ constexpr int kFinishRows = 8;
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                           int64_t w_stride, SweepParts parts, T* __restrict__ dx, int64_t dx_stride) {
-    constexpr int HELD = kSweepHeld;
+    constexpr int HELD = sweep_shape(MODE, D).held();
     constexpr int PER = D / 64;     // numbers of a lane
     constexpr int kAtOnce = 5;      // labels' rows under way
     const int64_t live = a.header->n_live;
-    const SweepDeal deal(live, HELD, a.V, sweep_unit(MODE, D));
+    const SweepDeal deal(live, a.V, sweep_shape(MODE, D));
     const int e0 = lane_id() * PER;
     for (int64_t p0 = (int64_t)blockIdx.x * kFinishRows; p0 < live; p0 += (int64_t)gridDim.x * kFinishRows) {
         const int64_t tile = p0 / HELD, x0 = tile * deal.units;
@@ -573,7 +580,7 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
     if (kLds > 64 * 1024)
         ND_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&sweep_kernel<T, D, MODE>),
                                          hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
-    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(kSweepGroups), dim3(Shape<MODE, D>::kThreads), kLds, stream, a, s);
+    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(sweep_shape(MODE, D).groups()), dim3(Shape<MODE, D>::kThreads), kLds, stream, a, s);
     ND_HIP_CHECK(hipGetLastError());
     return ND_OK;
 }
@@ -581,8 +588,9 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
 }  // namespace
 
 int sweep_width(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : d <= 256 ? 256 : 0; }
-int64_t sweep_segments(int mode, int64_t held) {
-    return mode == kSweepDw ? 2 * kSweepGroups : kSweepGroups + (held + kSweepHeld - 1) / kSweepHeld;
+int64_t sweep_rows(int mode, int64_t held, int32_t dp) {
+    const SweepShape shape = sweep_shape(mode, dp);
+    return (mode == kSweepDw ? 2 * shape.groups() : shape.groups() + (held + shape.held() - 1) / shape.held()) * shape.held();
 }
 
 template <typename T>
