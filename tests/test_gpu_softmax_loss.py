@@ -255,6 +255,44 @@ def test_step_arrays_of_walks_are_labels():
     Loss(rows.cpu(), table.cpu(), steps[3].cpu()).check(*out)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("V,d", [(1, 128), (63, 5), (4097, 128), (1000, 8), (70000, 60), (3000, 1024), (257, 1001), (100, 7)])
+def test_few_rows_forward(n, V, d, kind):
+    """Serving: one centre or a handful, over any number of vertices."""
+    x, w, labels, _ = _inputs(n, V, d, 3, TYPES[kind], seed=n + V, empty=0.0)
+    if n > 2:
+        labels[1] = -1
+        x[1] = float("nan")
+    out = _run(x.to(DEV), w.to(DEV), labels.to(DEV), None, grad=False)
+    Loss(x, w, labels).check(*out)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("d", [128, 300])
+@pytest.mark.parametrize("n", [3, 200])
+def test_vertices_that_scores_rule_out(n, d, kind):
+    """Scores of the type's lowest values, or of minus infinity (forward), as programs mask vertices with: as if they were
+    not there."""
+    V = 700
+    x, w, labels, row_weight = _inputs(n, V, d, 2, TYPES[kind], seed=43)
+    x[:, 0] = 1.0
+    out_of_it = torch.zeros(V, dtype=torch.bool)
+    out_of_it[:300] = True
+    labels = torch.where(labels >= 0, labels % 400 + 300, labels)
+    kept = Loss(x, w[~out_of_it], torch.where(labels >= 0, labels - 300, labels), row_weight)
+    low = torch.finfo(w.dtype).min if kind != "f16" else -30000.0
+    for value, grad in ((low, True), (low, False), (float("-inf"), False)):
+        masked = w.clone()
+        masked[out_of_it] = 0
+        masked[out_of_it, 0] = value
+        out = _run(x.to(DEV), masked.to(DEV), labels.to(DEV), row_weight.to(DEV), grad)
+        kept.check(*out[:2], what=f"{value}")
+        if grad:
+            kept.check(*out[:2], out[2], out[3][~out_of_it.to(DEV)], what=f"{value}")
+            assert not bool(out[3][out_of_it.to(DEV)].any())
+
+
 def test_refusals():
     x, w = torch.zeros(4, 8, device=DEV), torch.zeros(9, 8, device=DEV)
     labels, f = torch.zeros(4, 2, dtype=torch.int32, device=DEV), torch.zeros(4, device=DEV)
