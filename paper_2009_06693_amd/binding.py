@@ -169,6 +169,9 @@ def lib() -> ctypes.CDLL:
                                     "`python -m paper_2009_06693_amd.build`") from e
         _nd_call.init(*(ctypes.cast(f, vp).value for f in (L.nd_sample, L.nd_sample_static, L.nd_samples_pack)),
                       ctypes.sizeof(nd_params))
+        _nd_call.init_rows(*(ctypes.cast(f, vp).value for f in (
+            L.nd_softmax_loss, L.nd_softmax_loss_grad, L.nd_group_positions, L.nd_rows_by_transit, L.nd_rows_to_samples,
+            L.nd_rows_weight_grad, L.nd_rows_group_sum_workspace_bytes, L.nd_rows_group_sum)))
         _call = _nd_call
         _lib = L
     return _lib
@@ -425,45 +428,28 @@ def layer_edges(g: Graph, transits: torch.Tensor, sampled: torch.Tensor, stream=
 # Rows of features: 2-D CUDA tensors of float32, bfloat16 or float16 whose rows lie in one piece, at any stride.
 # ---------------------------------------------------------------------------
 
-def _on_device(t, what: str, dtype=None, entries: Optional[int] = None):
-    """The address of a contiguous tensor on the current device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
-        raise TypeError(f"{what} must be a contiguous CUDA tensor" + (f" of {dtype}" if dtype is not None else ""))
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{what} lies on device {t.get_device()} but device {torch.cuda.current_device()} is current")
-    if entries is not None and t.numel() < entries:
-        raise ValueError(f"{what} has {t.numel()} entries, {entries} are needed")
-    return t.data_ptr()
+def _place(stream: Optional[torch.cuda.Stream]):
+    """The current device and the address of the stream a call goes to."""
+    device = torch.cuda.current_device()
+    return device, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _rows(t, what: str, dtype=None, d: Optional[int] = None, n: Optional[int] = None):
-    """(address, stride) of rows."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype not in _ROW_TYPES:
-        raise TypeError(f"{what} must be a 2-D CUDA tensor of float32, bfloat16 or float16")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{what} lies on device {t.get_device()} but device {torch.cuda.current_device()} is current")
-    rows, cols = t.shape
-    if (dtype is not None and t.dtype != dtype) or (d is not None and cols != d) or (n is not None and rows != n):
-        raise ValueError(f"{what} is {rows} x {cols} of {t.dtype}, expected {rows if n is None else n} x "
-                         f"{cols if d is None else d} of {t.dtype if dtype is None else dtype}")
-    stride, step = t.stride()
-    if cols > 1 and step != 1:
-        raise ValueError(f"{what}: the numbers of a row must lie next to each other")
-    if rows > 1 and stride < cols:
-        raise ValueError(f"{what}: rows must not overlap")
-    return t.data_ptr(), (stride if rows > 1 else max(cols, 1))
+def _made(result):
+    if type(result) is int:
+        _check(result)
+    return result
 
 
-def _new(shape, dtype, device, stream):
-    """Memory for a call on that stream: in the stream's own order, so that what its last owner still does to it is over."""
+def _rows_call(name: str, stream, *args):
+    """What a call of _nd_call makes; on a stream of its own the memory it makes comes in that stream's order, so that what
+    the last owner still does to it is over."""
+    if _call is None:
+        lib()
+    call = getattr(_call, name)
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _made(call(*args, *_place(None)))
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _optional(t, what: str, dtype, entries: int):
-    return None if t is None else _on_device(t, what, dtype, entries)
+        return _made(call(*args, *_place(stream)))
 
 
 def nd_softmax_loss_workspace_bytes(n: int, V: int, d: int, k: int, dtype: torch.dtype, grad: bool) -> int:
@@ -474,109 +460,47 @@ def nd_softmax_loss_workspace_bytes(n: int, V: int, d: int, k: int, dtype: torch
     return size
 
 
-def _loss_args(x, w, labels, loss, lse):
-    xp, xs = _rows(x, "x")
-    wp, wst = _rows(w, "w", x.dtype, x.shape[1])
-    n, d = x.shape
-    if not isinstance(labels, torch.Tensor) or labels.dim() not in (1, 2) or labels.shape[0] != n:
-        raise ValueError("labels must hold one row of labels per row of x")
-    k = labels.shape[1] if labels.dim() == 2 else 1
-    return (xp, xs, wp, wst, _ROW_TYPES[x.dtype], n, w.shape[0], d, _on_device(labels, "labels", torch.int32), k,
-            _on_device(loss, "loss", torch.float32, n), _on_device(lse, "lse", torch.float32, n))
-
-
 def nd_softmax_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
                     workspace: torch.Tensor, stream=None):
     """x [n, d], w [V, d], labels int32 [n] or [n, k]; loss and lse float32 [n] are written."""
-    xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep = _loss_args(x, w, labels, loss, lse)
-    _check(lib().nd_softmax_loss(xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep, _on_device(workspace, "workspace"),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    _rows_call("softmax_loss", stream, x, w, labels, loss, lse, workspace)
 
 
 def nd_softmax_loss_grad(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, row_weight: Optional[torch.Tensor],
                          loss: torch.Tensor, lse: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor],
                          workspace: torch.Tensor, stream=None):
     """As nd_softmax_loss; row_weight float32 [n] or None; dx [n, d] and dw [V, d] are written (None: not wanted)."""
-    xp, xs, wp, wst, dt, n, V, d, lp, k, op, ep = _loss_args(x, w, labels, loss, lse)
-    dxp, dxs = (None, d) if dx is None else _rows(dx, "dx", x.dtype, d, n)
-    dwp, dws = (None, d) if dw is None else _rows(dw, "dw", x.dtype, d, V)
-    _check(lib().nd_softmax_loss_grad(xp, xs, wp, wst, dt, n, V, d, lp, k,
-                                      _optional(row_weight, "row_weight", torch.float32, n), op, ep, dxp, dxs, dwp, dws,
-                                      _on_device(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                      _stream_ptr(stream)))
+    _rows_call("softmax_loss_grad", stream, x, w, labels, loss, lse, workspace, row_weight, dx, dw)
 
 
 def nd_softmax_loss_status(workspace: torch.Tensor, stream=None):
     _check(lib().nd_softmax_loss_status(workspace.data_ptr(), _stream_ptr(stream)))
 
 
-def _slots_of(n: int, m: int, t, what: str, dtype):
-    return None if t is None else _on_device(t, what, dtype, n * m)
-
-
-def _pairs(sorted_slots, counts):
-    return (_on_device(sorted_slots, "sorted_slots", torch.int32), sorted_slots.numel(),
-            _optional(counts, "counts", torch.int64, 2))
-
-
 def nd_group_positions(sorted_slots: torch.Tensor, n_slots: int, counts: Optional[torch.Tensor] = None,
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Where every slot's pair lies in sorted_slots (int32 [n_slots], -1: in no pair).  counts: what the grouping left on
-    the device, where sorted_slots has room for more pairs than are live."""
-    sp, pairs, cp = _pairs(sorted_slots, counts)
-    if out is None:
-        out = _new(n_slots, torch.int32, sorted_slots.device, stream)
-    _check(lib().nd_group_positions(sp, pairs, cp, n_slots, _on_device(out, "out", torch.int32, n_slots),
-                                    _stream_ptr(stream)))
-    return out
+    the device (int64 [2]), where sorted_slots has room for more pairs than are live."""
+    return _rows_call("positions", stream, sorted_slots, n_slots, counts, out)
 
 
 def nd_rows_by_transit(x: torch.Tensor, sorted_slots: torch.Tensor, m: int, weights: Optional[torch.Tensor] = None,
                        counts: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        stream=None) -> torch.Tensor:
     """Rows in the order of the groups: out[p] = weights[q] * x[q // m], q = sorted_slots[p].  weights float32 [n * m]."""
-    xp, xs = _rows(x, "x")
-    sp, pairs, cp = _pairs(sorted_slots, counts)
-    n, d = x.shape
-    if out is None:
-        out = _new((pairs, d), x.dtype, x.device, stream)
-    op, ost = _rows(out, "out", x.dtype, d, pairs)
-    _check(lib().nd_rows_by_transit(xp, xs, _ROW_TYPES[x.dtype], n, d, sp, pairs, cp, m,
-                                    _slots_of(n, m, weights, "weights", torch.float32), op, ost, _stream_ptr(stream)))
-    return out
-
-
-def _samples(index: torch.Tensor, m: int):
-    if m < 1 or not isinstance(index, torch.Tensor) or index.numel() % m != 0:
-        raise ValueError(f"index must hold {m} slots per row")
-    return _on_device(index, "index", torch.int32), index.numel() // m
+    return _rows_call("by_transit", stream, x, sorted_slots, m, weights, counts, out)
 
 
 def nd_rows_to_samples(z: torch.Tensor, index: torch.Tensor, m: int, weights: Optional[torch.Tensor] = None,
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[r] = sum over j of weights[r * m + j] * z[index[r * m + j]]; places outside [0, len(z)) are skipped."""
-    zp, zs = _rows(z, "z")
-    ip, n = _samples(index, m)
-    d = z.shape[1]
-    if out is None:
-        out = _new((n, d), z.dtype, z.device, stream)
-    op, ost = _rows(out, "out", z.dtype, d, n)
-    _check(lib().nd_rows_to_samples(zp, zs, _ROW_TYPES[z.dtype], z.shape[0], d, ip, n, m,
-                                    _slots_of(n, m, weights, "weights", torch.float32), op, ost, _stream_ptr(stream)))
-    return out
+    return _rows_call("to_samples", stream, z, index, m, weights, out)
 
 
 def nd_rows_weight_grad(dy: torch.Tensor, z: torch.Tensor, index: torch.Tensor, m: int,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[r * m + j] = dy[r] . z[index[r * m + j]] (float32), 0 where nd_rows_to_samples skips."""
-    zp, zs = _rows(z, "z")
-    ip, n = _samples(index, m)
-    dyp, dys = _rows(dy, "dy", z.dtype, z.shape[1], n)
-    if out is None:
-        out = _new(n * m, torch.float32, z.device, stream)
-    _check(lib().nd_rows_weight_grad(dyp, dys, zp, zs, _ROW_TYPES[z.dtype], z.shape[0], z.shape[1], ip, n, m,
-                                     _on_device(out, "out", torch.float32, n * m), _stream_ptr(stream)))
-    return out
+    return _rows_call("weight_grad", stream, dy, z, index, m, out)
 
 
 def nd_rows_group_sum_workspace_bytes(n_pairs: int, d: int) -> int:
@@ -590,32 +514,8 @@ def nd_rows_group_sum(x: torch.Tensor, sorted_slots: torch.Tensor, group_start: 
                       stream=None) -> torch.Tensor:
     """Sums per group of weights[q] * x[q // m]; group_start int32 [groups + 1].  With group_rows (int32 [groups],
     ascending: the grouping's transits) the sums are those rows of a table of num_rows, whose other rows are 0."""
-    xp, xs = _rows(x, "x")
-    sp, pairs, cp = _pairs(sorted_slots, counts)
-    gp = _on_device(group_start, "group_start", torch.int32, 1)
-    n, d = x.shape
-    groups = group_start.numel() - 1
-    if group_rows is None:
-        num_rows = groups if out is None else out.shape[0]
-    elif num_rows is None and out is None:
-        raise ValueError("group_rows need num_rows or out")
-    elif num_rows is None:
-        num_rows = out.shape[0]
-    if out is None:
-        out = _new((num_rows, d), x.dtype, x.device, stream)
-    op, ost = _rows(out, "out", x.dtype, d, num_rows)
-    rp = _optional(group_rows, "group_rows", torch.int32, groups)
-    if group_rows is not None and groups == 0:
-        rp = op  # an empty tensor has no address; it is not read
-    wsb = nd_rows_group_sum_workspace_bytes(pairs, d)
-    if workspace is None:
-        workspace = _new(wsb, torch.uint8, x.device, stream)
-    _check(lib().nd_rows_group_sum(xp, xs, _ROW_TYPES[x.dtype], n, d, sp, pairs, gp, groups, cp, m,
-                                   _slots_of(n, m, weights, "weights", torch.float32),
-                                   rp, op, ost, num_rows,
-                                   _on_device(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                   _stream_ptr(stream)))
-    return out
+    return _rows_call("group_sum", stream, x, sorted_slots, group_start, m, weights, group_rows, num_rows, counts, out,
+                      workspace)
 
 
 class SoftmaxLoss:
