@@ -29,12 +29,13 @@ struct Deal {
     uint32_t rows;        // rows of a workgroup
     uint32_t lanes;       // rows * pieces
 };
-inline Deal make_deal(int32_t d, int vec) {
+inline Deal make_deal(int32_t d, int vec, uint32_t threads = kThreads) {
     Deal t;
     t.all_pieces = (uint32_t)((d + vec - 1) / vec);
-    const uint32_t here = t.all_pieces < kThreads ? t.all_pieces : kThreads;
+    const uint32_t most = threads < kThreads ? threads : kThreads;
+    const uint32_t here = t.all_pieces < most ? t.all_pieces : most;
     t.pieces = make_fastdiv(here);
-    t.rows = kThreads / here;
+    t.rows = threads / here;
     t.lanes = t.rows * here;
     return t;
 }
@@ -115,90 +116,149 @@ __global__ __launch_bounds__(kThreads) void by_transit_kernel(const T* __restric
     }
 }
 
-// A lane adds up its piece of the m rows, eight loads under way at a time.
+// A lane adds up its piece of every `step`-th slot's row from `first` on, four loads under way at a time (eight or sixteen take
+// registers from wavefronts: 199 and 253 us where four take 194, 233,000 rows of 25 slots x 128 bf16).
+constexpr int kAhead = 4;
+template <typename T, int VEC>
+__device__ __forceinline__ void add_slots(const T* __restrict__ z, int64_t z_stride, uint32_t n_z, const int32_t* idx,
+                                          const float* w, int32_t first, int32_t m, int32_t step, int32_t at,
+                                          float (&sum)[VEC]) {
+    for (int32_t j0 = first; j0 < m; j0 += kAhead * step) {
+        uint32_t place[kAhead];
+        Piece<T, VEC> v[kAhead];
+        float f[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) place[i] = j0 + i * step < m ? (uint32_t)idx[j0 + i * step] : ~0u;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            v[i] = Piece<T, VEC>{};
+            f[i] = 0.f;
+            if (place[i] < n_z) {
+                v[i] = load_piece<T, VEC>(z + (int64_t)place[i] * z_stride + at);
+                f[i] = w ? w[j0 + i * step] : 1.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] = fmaf(f[i], (float)v[i].v[e], sum[e]);
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_sum(T* __restrict__ to, const float (&sum)[VEC]) {
+    Piece<T, VEC> o;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
+    store_piece<T, VEC>(to, o);
+}
+
 template <typename T, int VEC>
 __global__ __launch_bounds__(kThreads) void to_samples_kernel(const T* __restrict__ z, int64_t z_stride, uint32_t n_z, int32_t d,
                                                               Deal t, const int32_t* __restrict__ index, int64_t n, int32_t m,
                                                               const float* __restrict__ weights, T* __restrict__ out,
                                                               int64_t out_stride) {
-    constexpr int kAhead = 8;
     uint32_t row;
     int32_t at;
     if (!deal_lane<VEC>(t, d, &row, &at)) return;
     for (int64_t r = (int64_t)blockIdx.x * t.rows + row; r < n; r += (int64_t)gridDim.x * t.rows) {
-        const int32_t* idx = index + r * m;
-        const float* w = weights ? weights + r * m : nullptr;
         float sum[VEC] = {};
-        for (int32_t j0 = 0; j0 < m; j0 += kAhead) {
-            uint32_t place[kAhead];
-            Piece<T, VEC> v[kAhead];
-            float f[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) place[i] = j0 + i < m ? (uint32_t)idx[j0 + i] : ~0u;
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                v[i] = Piece<T, VEC>{};
-                f[i] = 0.f;
-                if (place[i] < n_z) {
-                    v[i] = load_piece<T, VEC>(z + (int64_t)place[i] * z_stride + at);
-                    f[i] = w ? w[j0 + i] : 1.f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum[e] = fmaf(f[i], (float)v[i].v[e], sum[e]);
-        }
-        Piece<T, VEC> o;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
-        store_piece<T, VEC>(out + r * out_stride + at, o);
+        add_slots<T, VEC>(z, z_stride, n_z, index + r * m, weights ? weights + r * m : nullptr, 0, m, 1, at, sum);
+        store_sum<T, VEC>(out + r * out_stride + at, sum);
     }
 }
 
-// 2^log_lanes lanes of a wavefront share the dot products of one row with four of its slots' rows.
+// Few rows: the slots of one are shared out over the rows of a workgroup's lanes and joined in their order.
+constexpr uint32_t kShareThreads = 1024;
 template <typename T, int VEC>
+__global__ __launch_bounds__(kShareThreads) void to_samples_share_kernel(const T* __restrict__ z, int64_t z_stride, uint32_t n_z,
+                                                                         int32_t d, Deal t, const int32_t* __restrict__ index,
+                                                                         int32_t m, const float* __restrict__ weights,
+                                                                         T* __restrict__ out, int64_t out_stride) {
+    extern __shared__ float shared_sums[];
+    uint32_t row;
+    int32_t at;
+    const bool mine = deal_lane<VEC>(t, d, &row, &at);
+    const int64_t r = blockIdx.x;
+    float sum[VEC] = {};
+    if (mine)
+        add_slots<T, VEC>(z, z_stride, n_z, index + r * m, weights ? weights + r * m : nullptr, (int32_t)row, m, (int32_t)t.rows,
+                          at, sum);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) shared_sums[threadIdx.x * VEC + e] = sum[e];
+    __syncthreads();
+    if (!mine || row != 0) return;
+    for (uint32_t k = 1; k < t.rows; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] += shared_sums[(threadIdx.x + k * t.pieces.d) * VEC + e];
+    store_sum<T, VEC>(out + r * out_stride + at, sum);
+}
+
+// Of HELD sums over lanes the upper half of the lanes goes on with the upper half, the lower with the others; *first: the
+// first of what a lane goes on with.
+template <int HELD, int N>
+__device__ __forceinline__ void fold(float (&dot)[N], int lane, int* s, int* first) {
+    if constexpr (HELD > 1) {
+        const bool upper = lane & *s;
+#pragma unroll
+        for (int i = 0; i < HELD / 2; ++i) {
+            const float keep = upper ? dot[HELD / 2 + i] : dot[i], give = upper ? dot[i] : dot[HELD / 2 + i];
+            dot[i] = keep + __shfl_xor(give, *s);
+        }
+        if (upper) *first += HELD / 2;
+        *s >>= 1;
+        fold<HELD / 2>(dot, lane, s, first);
+    }
+}
+
+// 2^log_lanes lanes of a wavefront share the dot products of one row with SLOTS of its slots' rows, whose pieces are under
+// way together (four: 231 us for 233,000 rows of 25 slots x 128 bf16; eight 288).  In the first steps of the sum over the lanes, half of them go on with half of the products each.
+template <typename T, int VEC, int SLOTS>
 __global__ __launch_bounds__(kThreads) void weight_grad_kernel(const T* __restrict__ dy, int64_t dy_stride,
                                                                const T* __restrict__ z, int64_t z_stride, uint32_t n_z,
                                                                int32_t d, const int32_t* __restrict__ index, int64_t n,
-                                                               int32_t m, int32_t quads, int log_lanes,
+                                                               int32_t m, FastDiv shares, int log_lanes,
                                                                float* __restrict__ dweights) {
     const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
-    const int64_t per = kThreads >> log_lanes, items = n * quads;
+    const int64_t per = kThreads >> log_lanes, items = n * shares.d;
     for (int64_t i0 = (int64_t)blockIdx.x * per; i0 < items; i0 += (int64_t)gridDim.x * per) {
         const int64_t item = i0 + (threadIdx.x >> log_lanes);
         const bool mine = item < items;
-        const int64_t r = mine ? item / quads : 0;
-        const int32_t j0 = (int32_t)(item - r * quads) * 4;
-        uint32_t place[4];
+        const int64_t r = mine ? fastdiv((uint32_t)item, shares) : 0;
+        const int32_t j0 = (int32_t)(item - r * shares.d) * SLOTS;
+        uint32_t place[SLOTS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) place[i] = mine && j0 + i < m ? (uint32_t)index[r * m + j0 + i] : ~0u;
-        float dot[4] = {};
+        for (int i = 0; i < SLOTS; ++i) place[i] = mine && j0 + i < m ? (uint32_t)index[r * m + j0 + i] : ~0u;
+        float dot[SLOTS] = {};
         for (int32_t c = lane * VEC; mine && c < d; c += lanes * VEC) {
-            const int32_t at = c + VEC <= d ? c : d - VEC;  // the last piece reaches back; what was counted is skipped
-            const int32_t skip = c - at;
+            const int32_t at = c + VEC <= d ? c : d - VEC;
             const Piece<T, VEC> a = load_piece<T, VEC>(dy + r * dy_stride + at);
-            Piece<T, VEC> b[4];
+            Piece<T, VEC> b[SLOTS];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < SLOTS; ++i) {
                 b[i] = Piece<T, VEC>{};
                 if (place[i] < n_z) b[i] = load_piece<T, VEC>(z + (int64_t)place[i] * z_stride + at);
             }
+            if (c == at) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (place[i] >= n_z) continue;
+                for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (e >= skip) dot[i] = fmaf((float)a.v[e], (float)b[i].v[e], dot[i]);
+                    for (int e = 0; e < VEC; ++e) dot[i] = fmaf((float)a.v[e], (float)b[i].v[e], dot[i]);
+            } else {  // the last piece reaches back; what was counted is skipped
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (e >= c - at) dot[i] = fmaf((float)a.v[e], (float)b[i].v[e], dot[i]);
             }
         }
-        for (int s = lanes >> 1; s > 0; s >>= 1)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dot[i] += __shfl_xor(dot[i], s);
-        if (mine && lane == 0)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (j0 + i < m) dweights[r * m + j0 + i] = dot[i];
+        for (int i = 0; i < SLOTS; ++i)
+            if (place[i] >= n_z) dot[i] = 0.f;  // also where dy is infinite or no number
+        int s = lanes >> 1, first = 0;
+        fold<SLOTS>(dot, lane, &s, &first);
+        const int rest = (s << 1) - 1;  // lanes that hold parts of the same product
+        for (; s > 0; s >>= 1) dot[0] += __shfl_xor(dot[0], s);
+        if (mine && (rest <= 0 || (lane & rest) == 0) && j0 + first < m) dweights[r * m + j0 + first] = dot[0];
     }
 }
 
@@ -225,9 +285,8 @@ __device__ __forceinline__ int64_t row_of_group(const GroupSum& g, int64_t u) {
     return r >= 0 && r < g.out_rows ? r : -1;
 }
 
-__global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
-    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
-    const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+// Which group every tile begins in.
+__device__ __forceinline__ void mark_tiles(const GroupSum& g, int64_t groups, int64_t pairs, int64_t u) {
     int64_t first = 0, last = -1;  // tiles whose first pair is this group's
     if (u < groups) {
         const int64_t a = start_of(g, u, pairs), b = start_of(g, u + 1, pairs);
@@ -248,30 +307,75 @@ __global__ __launch_bounds__(kThreads) void group_tiles_kernel(GroupSum g) {
     }
 }
 
+// Rows that no group names are zero: a workgroup marks the named ones of 256 rows and clears the others.
+template <typename T, int VEC>
+__device__ __forceinline__ void clear_rows(const GroupSum& g, int64_t groups, int64_t pairs, int32_t d, const Deal& t,
+                                           int64_t r0, T* __restrict__ out) {
+    __shared__ uint32_t named[kThreads];
+    const int64_t r1 = r0 + kThreads < g.out_rows ? r0 + kThreads : g.out_rows;
+    int64_t lo = 0, hi = groups;  // first group with a row of r0 or more; every lane looks at one place at a time
+    while (lo < hi) {
+        const int64_t step = (hi - lo + kThreads - 1) / kThreads, at = lo + threadIdx.x * step;
+        const int64_t less = __syncthreads_count(at < hi && (int64_t)g.group_row[at] < r0);
+        hi = lo + less * step < hi ? lo + less * step : hi;
+        if (less > 0) lo += (less - 1) * step + 1;
+    }
+    named[threadIdx.x] = 0;
+    __syncthreads();
+    // rows ascend, so that at most as many groups as rows follow
+    const int64_t u = lo + threadIdx.x;
+    if (u < groups) {
+        const int64_t r = g.group_row[u];
+        const bool holds = start_of(g, u + 1, pairs) > start_of(g, u, pairs);
+        if (r >= r0 && r < r1 && holds) named[r - r0] = 1;
+    }
+    __syncthreads();
+    const uint32_t row = fastdiv(threadIdx.x, t.pieces);
+    if (threadIdx.x >= t.lanes) return;
+    for (uint32_t c = threadIdx.x - row * t.pieces.d; c < t.all_pieces; c += t.pieces.d) {
+        const int32_t at = (int32_t)(c + 1) * VEC <= d ? (int32_t)c * VEC : d - VEC;
+        for (int64_t r = r0 + row; r < r1; r += t.rows)
+            if (!named[r - r0]) store_piece<T, VEC>(out + r * g.out_stride + at, Piece<T, VEC>{});
+    }
+}
+
+// The first `tile_blocks` workgroups do the one, the others the other.
+template <typename T, int VEC>
+__global__ __launch_bounds__(kThreads) void group_tiles_kernel(int32_t d, Deal t, GroupSum g, int64_t tile_blocks,
+                                                               T* __restrict__ out) {
+    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
+    if (blockIdx.x < tile_blocks)
+        mark_tiles(g, groups, pairs, (int64_t)blockIdx.x * kThreads + threadIdx.x);
+    else
+        clear_rows<T, VEC>(g, groups, pairs, d, t, (blockIdx.x - tile_blocks) * kThreads, out);
+}
+
 template <typename T, typename O, int VEC, bool BY_ROW>
 __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict__ x, int64_t x_stride, int32_t d, Deal t,
                                                              FastDiv m, uint32_t n_slots,
                                                              const float* __restrict__ weights, GroupSum g,
                                                              O* __restrict__ out) {
-    constexpr int kAhead = 8;
     uint32_t row;
     int32_t at;
     if (!deal_lane<VEC>(t, d, &row, &at)) return;
-    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
+    const uint32_t groups = (uint32_t)live_groups(g), pairs = (uint32_t)grouped_pairs(g, groups);
     for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * g.tile < pairs; tile += (int64_t)gridDim.x * t.rows) {
-        const int64_t p0 = tile * g.tile;
-        const int64_t p1 = p0 + g.tile < pairs ? p0 + g.tile : pairs;
-        int64_t u = (uint32_t)g.tile_group[tile];
+        const uint32_t p0 = (uint32_t)(tile * g.tile);
+        const uint32_t p1 = pairs - p0 < (uint32_t)g.tile ? pairs : p0 + g.tile;
+        uint32_t u = (uint32_t)g.tile_group[tile];
         if (u >= groups) u = groups - 1;
         bool before = start_of(g, u, pairs) < p0;
-        int64_t end = start_of(g, u + 1, pairs);
+        // of this group and the next, so that no group waits for where it ends
+        uint32_t end = (uint32_t)start_of(g, u + 1, pairs), next = u + 1 < groups ? u + 1 : u,
+                 next_end = (uint32_t)start_of(g, next + 1, pairs);
+        int64_t to = row_of_group(g, u), next_to = row_of_group(g, next);
         float sum[VEC] = {};
-        for (int64_t p = p0; p < p1; p += kAhead) {
-            uint32_t q[kAhead];
+        uint32_t q[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) q[i] = (uint32_t)i < p1 - p0 ? (uint32_t)g.slots[p0 + i] : ~0u;
+        for (uint32_t p = p0; p < p1; p += kAhead) {
             Piece<T, VEC> v[kAhead];
             float f[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) q[i] = p + i < p1 ? (uint32_t)g.slots[p + i] : ~0u;
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 v[i] = Piece<T, VEC>{};
@@ -283,32 +387,30 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
                 }
             }
 #pragma unroll
+            for (int i = 0; i < kAhead; ++i) q[i] = (uint32_t)(kAhead + i) < p1 - p ? (uint32_t)g.slots[p + kAhead + i] : ~0u;
+#pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (p + i >= p1) break;
+                if ((uint32_t)i >= p1 - p) break;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] = fmaf(f[i], (float)v[i].v[e], sum[e]);
-                if (p + i + 1 < end && p + i + 1 < p1) continue;
+                const uint32_t after = p + i + 1;
+                if (after < end && after < p1) continue;
                 // the group ends here, or the tile does
                 if (!before && end <= p1) {
-                    const int64_t r = row_of_group(g, u);
-                    if (r >= 0) {
-                        Piece<O, VEC> o;
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) o.v[e] = (O)sum[e];
-                        store_piece<O, VEC>(out + r * g.out_stride + at, o);
-                    }
+                    if (to >= 0) store_sum<O, VEC>(out + to * g.out_stride + at, sum);
                 } else {
-                    Piece<float, VEC> o;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) o.v[e] = sum[e];
-                    store_piece<float, VEC>(g.parts + (tile * 2 + (before ? 0 : 1)) * d + at, o);
+                    store_sum<float, VEC>(g.parts + (tile * 2 + (before ? 0 : 1)) * d + at, sum);
                 }
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
                 before = false;
-                while (end <= p + i + 1 && u + 1 < groups) {  // groups without pairs are passed over
-                    ++u;
-                    end = start_of(g, u + 1, pairs);
+                while (end <= after && u + 1 < groups) {  // groups without pairs are passed over
+                    u = next;
+                    end = next_end;
+                    to = next_to;
+                    next = u + 1 < groups ? u + 1 : u;
+                    next_end = (uint32_t)start_of(g, next + 1, pairs);
+                    next_to = row_of_group(g, next);
                 }
             }
         }
@@ -318,11 +420,7 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
 template <typename T, int VEC>
 __device__ __forceinline__ void store_group(const GroupSum& g, int64_t u, int32_t at, const float (&sum)[VEC], T* __restrict__ out) {
     const int64_t r = row_of_group(g, u);
-    if (r < 0) return;
-    Piece<T, VEC> o;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) o.v[e] = (T)sum[e];
-    store_piece<T, VEC>(out + r * g.out_stride + at, o);
+    if (r >= 0) store_sum<T, VEC>(out + r * g.out_stride + at, sum);
 }
 
 // Adds up what tiles left of a group.
@@ -386,45 +484,11 @@ __global__ __launch_bounds__(kThreads) void group_join_kernel(int32_t d, Deal t,
     }
 }
 
-// Rows that no group names are zero: a workgroup marks the named ones of 256 rows and clears the others.
-template <typename T, int VEC>
-__global__ __launch_bounds__(kThreads) void group_clear_kernel(int32_t d, GroupSum g, T* __restrict__ out) {
-    __shared__ uint32_t named[kThreads];
-    const int64_t groups = live_groups(g), pairs = grouped_pairs(g, groups);
-    const int64_t r0 = (int64_t)blockIdx.x * kThreads;
-    const int64_t r1 = r0 + kThreads < g.out_rows ? r0 + kThreads : g.out_rows;
-    int64_t lo = 0, hi = groups;  // first group with a row of r0 or more
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if ((int64_t)g.group_row[mid] < r0)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    named[threadIdx.x] = 0;
-    __syncthreads();
-    // rows ascend, so that at most as many groups as rows follow
-    const int64_t u = lo + threadIdx.x;
-    if (u < groups) {
-        const int64_t r = g.group_row[u];
-        const bool holds = start_of(g, u + 1, pairs) > start_of(g, u, pairs);
-        if (r >= r0 && r < r1 && holds) named[r - r0] = 1;
-    }
-    __syncthreads();
-    const int32_t per_row = (d + VEC - 1) / VEC;
-    for (int64_t r = r0 + wave_id(); r < r1; r += kThreads / kWave) {
-        if (named[r - r0]) continue;
-        for (int32_t c = lane_id(); c < per_row; c += kWave) {
-            const int32_t at = c * VEC + VEC <= d ? c * VEC : d - VEC;
-            store_piece<T, VEC>(out + r * g.out_stride + at, Piece<T, VEC>{});
-        }
-    }
-}
-
 // ------------------------------------------------------------------------------------------------------ launches
 // Pairs of a tile: few enough that 2,048 wavefronts, eight per compute unit, have one, since a tile's rows are fetched
-// eight at a time one after the other; more where there are enough, since a tile leaves up to two rows of floats.
-constexpr int32_t kLeastTile = 8, kMostTile = 64;
+// four at a time one after the other; more where there are enough, since a tile leaves up to two rows of floats (5.8
+// million pairs x 128 bf16: tiles of 64 pairs 333 us and 40 to join them, of 128 333 and 21, of 256 394 and 15).
+constexpr int32_t kLeastTile = 8, kMostTile = 128;
 int32_t tile_pairs(int64_t n_pairs, int32_t d, int bytes) {
     const int vec = d * bytes >= 16 ? 16 / bytes : 1;
     const int64_t pieces = (d + vec - 1) / vec;
@@ -455,13 +519,16 @@ int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t
     const Deal t = make_deal(d, VEC);
     g.tile = tile_pairs(g.n_pairs, d, (int)sizeof(T));
     const int64_t tiles = (g.n_pairs + g.tile - 1) / g.tile;
-    if (g.n_groups > 0 && tiles > 0) {
-        hipLaunchKernelGGL(group_tiles_kernel, dim3((unsigned)((g.n_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                           stream, g);
+    const bool sums = g.n_groups > 0 && tiles > 0;
+    const int64_t tile_blocks = sums ? (g.n_groups + kThreads - 1) / kThreads : 0;
+    const int64_t clear_blocks = g.group_row ? (g.out_rows + kThreads - 1) / kThreads : 0;
+    if (tile_blocks + clear_blocks > 0)
+        hipLaunchKernelGGL((group_tiles_kernel<O, VEC>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(kThreads), 0, stream, d,
+                           t, g, tile_blocks, out);
+    if (sums)
         hipLaunchKernelGGL((group_sum_kernel<T, O, VEC, BY_ROW>), dim3(workgroups((tiles + t.rows - 1) / t.rows), deal_columns(t)),
                            dim3(deal_threads(t)), 0, stream, x, x_stride, d, t, make_fastdiv((uint32_t)m), (uint32_t)(n * m),
                            weights, g, out);
-    }
     if (g.n_groups > 0)
         hipLaunchKernelGGL((group_join_kernel<O, VEC>), dim3(workgroups((g.n_groups + kWave - 1) / kWave), deal_columns(t)),
                            dim3(deal_threads(t)), 0, stream, d, t, g, out);
@@ -594,6 +661,19 @@ int nd_rows_to_samples(const void* z_dev, int64_t z_stride, int dtype, int64_t n
         return by_width<T>(d, [&](auto width) -> int {
             constexpr int VEC = decltype(width)::value;
             const Deal t = make_deal(d, VEC);
+            // Up to 2,048 wavefronts of rows, eight per compute unit, a row's slots are shared out: 1 row of 30,000 slots x 128
+            // bf16 199 us (5,510 with lanes that add up a row each), 200 rows of 30 3.9 (9.7), 6,000 rows of 30, just below,
+            // 10.7 (15.3).  Above, lanes are busy without it.
+            if (m > kAhead && n * t.all_pieces < 2048 * kWave) {
+                uint32_t threads = kWave;
+                while (threads < kShareThreads && (int64_t)threads * kAhead < (int64_t)m * t.all_pieces) threads *= 2;
+                const Deal share = make_deal(d, VEC, threads);
+                hipLaunchKernelGGL((to_samples_share_kernel<T, VEC>), dim3((unsigned)n, deal_columns(share)), dim3(threads),
+                                   threads * VEC * sizeof(float), stream, (const T*)z_dev, z_stride, (uint32_t)n_z, d, share,
+                                   index_dev, m, weights_dev, (T*)out_dev, out_stride);
+                ND_HIP_CHECK(hipGetLastError());
+                return ND_OK;
+            }
             hipLaunchKernelGGL((to_samples_kernel<T, VEC>), dim3(workgroups((n + t.rows - 1) / t.rows), deal_columns(t)),
                                dim3(deal_threads(t)), 0, stream, (const T*)z_dev, z_stride, (uint32_t)n_z, d, t, index_dev,
                                n, m, weights_dev, (T*)out_dev, out_stride);
@@ -621,13 +701,14 @@ int nd_rows_weight_grad(const void* dy_dev, int64_t dy_stride, const void* z_dev
         using T = std::remove_pointer_t<decltype(type)>;
         return by_width<T>(d, [&](auto width) -> int {
             constexpr int VEC = decltype(width)::value;
-            int log_lanes = 0;
-            while (log_lanes < 6 && (VEC << log_lanes) < d) ++log_lanes;
-            const int32_t quads = (m + 3) / 4;
+            constexpr int SLOTS = 4;
+            int log_lanes = 0;  // at least as many lanes as slots, which the sum over them expects
+            while ((1 << log_lanes) < SLOTS || (log_lanes < 6 && (VEC << log_lanes) < d)) ++log_lanes;
+            const int32_t shares = (m + SLOTS - 1) / SLOTS;
             const int64_t per = kThreads >> log_lanes;
-            hipLaunchKernelGGL((weight_grad_kernel<T, VEC>), dim3(workgroups((n * quads + per - 1) / per)), dim3(kThreads),
-                               0, stream, (const T*)dy_dev, dy_stride, (const T*)z_dev, z_stride, (uint32_t)n_z, d, index_dev,
-                               n, m, quads, log_lanes, dweights_dev);
+            hipLaunchKernelGGL((weight_grad_kernel<T, VEC, SLOTS>), dim3(workgroups((n * shares + per - 1) / per)),
+                               dim3(kThreads), 0, stream, (const T*)dy_dev, dy_stride, (const T*)z_dev, z_stride, (uint32_t)n_z,
+                               d, index_dev, n, m, make_fastdiv((uint32_t)shares), log_lanes, dweights_dev);
             ND_HIP_CHECK(hipGetLastError());
             return ND_OK;
         });
@@ -688,11 +769,6 @@ int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n,
         using T = std::remove_pointer_t<decltype(type)>;
         return by_width<T>(d, [&](auto width) -> int {
             constexpr int VEC = decltype(width)::value;
-            if (group_row_dev) {
-                hipLaunchKernelGGL((group_clear_kernel<T, VEC>), dim3((unsigned)((out_rows + kThreads - 1) / kThreads)),
-                                   dim3(kThreads), 0, stream, d, g, (T*)out_dev);
-                ND_HIP_CHECK(hipGetLastError());
-            }
             return launch_group_sum<T, T, VEC, false>((const T*)x_dev, x_stride, n, d, m, weights_dev, g, (T*)out_dev, stream);
         });
     });

@@ -81,6 +81,32 @@ def test_sums_over_sampled_vertices_and_their_gradient(n, m, V, d, kind):
         assert_within(B.nd_rows_group_sum(*args, fd, group_rows=ids.to(DEV), out=out), whole, allowed, "table")
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,m,d", [(1, 65536, 128), (2, 1000, 5), (3, 9, 2056), (1, 8, 64), (65, 17, 200), (16500, 12, 128),
+                                   (140000, 9, 3)])
+def test_slots_of_few_rows_and_of_many(n, m, d, kind):
+    dtype = TYPES[kind]
+    g = torch.Generator().manual_seed(n + m)
+    V = 97
+    table, dy = torch.randn(V, d, generator=g).to(dtype).to(DEV), torch.randn(n, d, generator=g).to(dtype).to(DEV)
+    index = torch.randint(-1, V + 1, (n * m,), generator=g).int().to(DEV)
+    weights = (torch.rand(n * m, generator=g) - 0.3).to(DEV)
+    print(f"[rows] slots n={n} m={m} d={d} {kind}", flush=True)
+    # sums over the slots of equal vertices first: 64-bit weights per row and vertex
+    live = (index >= 0) & (index < V)
+    at = torch.arange(n * m, device=DEV) // m * V + index.long().clamp(0, V - 1)
+    for w in (weights, None):
+        f = (torch.ones_like(weights) if w is None else weights).double() * live
+        per = torch.zeros(n * V, dtype=torch.float64, device=DEV).index_add_(0, at, f).view(n, V)
+        size = torch.zeros(n * V, dtype=torch.float64, device=DEV).index_add_(0, at, f.abs()).view(n, V)
+        want, sizes = per @ table.double(), size @ table.double().abs()
+        got = B.nd_rows_to_samples(table, index, m, w)
+        assert_within(got, want, rounded(want, (m + 1) * U32 * sizes, dtype), "sums")
+    dots, sizes = dy.double() @ table.double().T, dy.double().abs() @ table.double().abs().T
+    want, allowed = dots.view(-1)[at] * live, (d + 2) * U32 * sizes.view(-1)[at]
+    assert_within(B.nd_rows_weight_grad(dy, table, index, m), want, allowed, "weights' gradient")
+
+
 @pytest.mark.parametrize("sizes", [[1], [64], [65], [63, 1], [64, 64], [1, 63, 1, 128, 5], [0, 3, 0, 0, 200, 0], [1000, 1], [1] * 300,
                                    [129] * 20, [20000, 7], [5, 70000]])
 def test_groups_that_end_inside_and_across_tiles(sizes):
