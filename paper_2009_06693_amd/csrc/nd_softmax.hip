@@ -21,7 +21,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = 128;         // rows of a product's tile
 constexpr int kChunk = 16;         // bytes that a lane moves at once
-constexpr size_t kPieceBytes = 512u << 20;  // probabilities that lie in the workspace at a time
+constexpr size_t kPieceBytes = (size_t)512 << 20;  // probabilities that lie in the workspace at a time, where scores are not kept
+constexpr int64_t kKeptBytes = (int64_t)4 << 30;    // scores that are kept at most,
+constexpr int64_t kCachedBytes = (int64_t)160 << 20;  // and where the cache holds them with what is made of them
 
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef short Short4 __attribute__((ext_vector_type(4)));
@@ -415,8 +417,10 @@ __device__ __forceinline__ int64_t tile_id() {
 
 // ------------------------------------------------------------------------------------------------------- forward
 // A workgroup takes 128 rows and every groups-th tile of 256 vertices; a lane keeps maximum and sum of its two columns.
+// scores (may be null): the products themselves, as [vertex][row].
 template <typename T>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x) {
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x,
+                                                         float* __restrict__ scores) {
     __shared__ __align__(16) char lds[kLdsBytes];
     const int64_t id = tile_id(), blocks = a.n_pad / kTile, group = id / blocks, n0 = id % blocks * kTile;
     if (n0 >= (int64_t)a.header->n_live) return;
@@ -433,6 +437,21 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (i * 32 + 8 * (r / 4) + r % 4 >= left) acc[i][j][r] = -INFINITY;
+        }
+        if (scores) {
+            // the row's address is the wavefront's, where in it the lane's: one register for all stores
+            const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+            float* at = scores + (v0 + wave / 2 * 128) * a.n_pad + n0 + wave % 2 * 64;
+            const uint32_t lane = (uint32_t)(lane_id() >> 5) * 4u * (uint32_t)a.n_pad + (lane_id() & 31);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    at[lane] = acc[i][0][r];
+                    at[lane + 32] = acc[i][1][r];
+                    at += (r % 4 == 3 ? 5 : 1) * a.n_pad;
+                    asm volatile("" : "+s"(at));
+                }
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -653,28 +672,33 @@ __global__ __launch_bounds__(kThreads) void few_finish_kernel(LossArgs a, const 
 }
 
 // ------------------------------------------------------------------------------------------------------ gradient
+// How often each of 256 vertices from v0 on is among the labels of 128 places from n0 on: counts[place][vertex], a lane a
+// place.
+constexpr int kCountPitch = kTileM + 4;
+__device__ __forceinline__ void count_labels(const LossArgs& a, int64_t v0, int64_t n0, uint8_t* counts) {
+    if (threadIdx.x < kTile) {
+        uint8_t* mine = counts + threadIdx.x * kCountPitch;
+        for (int e = 0; e < kTileM / 4; ++e) reinterpret_cast<uint32_t*>(mine)[e] = 0;
+        for (int32_t j = 0; j < a.k; ++j) {
+            const int64_t v = a.labels_of[(n0 + threadIdx.x) * a.k + j];
+            if (v >= v0 && v < v0 + kTileM) mine[v - v0]++;
+        }
+    }
+    __syncthreads();
+}
+
 // g (c p - count) of 256 vertices of the piece from v_first on and 128 rows, as [vertex][row].
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
                                                          T* __restrict__ probs) {
     __shared__ __align__(16) char lds[kLdsBytes];
-    constexpr int kPitch = kTileM + 4;
     const int64_t id = tile_id(), blocks = a.n_pad / kTile;
     const int64_t n0 = id % blocks * kTile, m0 = id / blocks * kTileM, v0 = v_first + m0;
     if (n0 >= (int64_t)a.header->n_live) return;
     AccTile acc;
     product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
-    // how often a vertex is among a row's labels: a lane owns a row's 256 counts
     uint8_t* counts = reinterpret_cast<uint8_t*>(lds);
-    if (threadIdx.x < kTile) {
-        uint32_t* mine = reinterpret_cast<uint32_t*>(counts + threadIdx.x * kPitch);
-        for (int e = 0; e < kTileM / 4; ++e) mine[e] = 0;
-        for (int32_t j = 0; j < a.k; ++j) {
-            const int64_t v = a.labels_of[(n0 + threadIdx.x) * a.k + j];
-            if (v >= v0 && v < v0 + kTileM) counts[threadIdx.x * kPitch + (v - v0)]++;
-        }
-    }
-    __syncthreads();
+    count_labels(a, v0, n0, counts);
     const float scale = a.header->scale;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -685,10 +709,46 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int row = acc_row(i, r);
-                const float held = (float)counts[col * kPitch + row];
+                const float held = (float)counts[col * kCountPitch + row];
                 const float p = v0 + row < a.V && c > 0.f ? g * (c * exp_of(acc[i][j][r] - lse) - held) : 0.f;
                 probs[(m0 + row) * a.n_pad + n0 + col] = (T)p;
             }
+    }
+}
+
+// The same from scores that were kept; fp32: in their place.  A lane has four places.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float* scores, T* probs) {
+    __shared__ __align__(16) uint8_t counts[kTile * kCountPitch];
+    constexpr int kLanes = kTile / 4, kRows = kThreads / kLanes, kAtOnce = 8;
+    const int64_t id = tile_id(), blocks = a.n_pad / kTile;
+    const int64_t n0 = id % blocks * kTile, v0 = id / blocks * kTileM;
+    if (n0 >= (int64_t)a.header->n_live) return;
+    count_labels(a, v0, n0, counts);
+    const float scale = a.header->scale;
+    const int col = threadIdx.x % kLanes * 4, first = threadIdx.x / kLanes;
+    float lse[4], c[4], g[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        lse[e] = a.place_lse[n0 + col + e];
+        c[e] = a.count[n0 + col + e];
+        g[e] = a.weight[n0 + col + e] * scale;
+    }
+    for (int r0 = first; r0 < kTileM; r0 += kRows * kAtOnce) {
+        Piece<float, 4> s[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) s[i] = load_piece<float, 4>(scores + (v0 + r0 + i * kRows) * a.n_pad + n0 + col);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int row = r0 + i * kRows;
+            Piece<T, 4> p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float held = (float)counts[(col + e) * kCountPitch + row];
+                p.v[e] = (T)(v0 + row < a.V && c[e] > 0.f ? g[e] * (c[e] * exp_of(s[i].v[e] - lse[e]) - held) : 0.f);
+            }
+            store_piece<T, 4>(probs + (v0 + row) * a.n_pad + n0 + col, p);
+        }
     }
 }
 
@@ -724,18 +784,47 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
             }
     }
 }
+// Four numbers of a row, summed over the shares' parts: a wavefront has 256 numbers of one row, eight parts under way.
+template <typename T>
+__device__ __forceinline__ void join_parts(const float* __restrict__ parts, int32_t shares, int64_t share_size, float back,
+                                           int32_t e, int32_t d, T* __restrict__ to) {
+    constexpr int kAtOnce = 8;
+    float sum[4] = {};
+    for (int32_t s0 = 0; s0 < shares; s0 += kAtOnce) {
+        Piece<float, 4> v[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            v[i] = Piece<float, 4>{};
+            if (s0 + i < shares) v[i] = load_piece<float, 4>(parts + (s0 + i) * share_size + e);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[q] += v[i].v[q];
+    }
+    Piece<T, 4> o;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o.v[q] = (T)(sum[q] * back);
+    if (e + 4 <= d) {
+        store_piece<T, 4>(to + e, o);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (e + q < d) to[e + q] = o.v[q];
+    }
+}
+constexpr int kJoinWidth = kWave * 4;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
                                                            int64_t part_rows, int64_t v_first, int64_t here, T* __restrict__ dw,
                                                            int64_t dw_stride) {
     const float back = 1.f / a.header->scale;
-    for (int64_t m = (int64_t)blockIdx.x * 4 + wave_id(); m < here; m += (int64_t)gridDim.x * 4)
-        for (int32_t e = lane_id(); e < a.d; e += kWave) {
-            float sum = 0.f;
-#pragma unroll 4
-            for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * part_rows + m) * a.dp + e];
-            dw[(v_first + m) * dw_stride + e] = (T)(sum * back);
-        }
+    const int32_t across = (a.d + kJoinWidth - 1) / kJoinWidth;
+    for (int64_t i = (int64_t)blockIdx.x * 4 + wave_id(); i < here * across; i += (int64_t)gridDim.x * 4) {
+        const int64_t m = i / across;
+        const int32_t e = (int32_t)(i - m * across) * kJoinWidth + lane_id() * 4;
+        if (e < a.d) join_parts<T>(parts + m * a.dp, shares, part_rows * a.dp, back, e, a.d, dw + (v_first + m) * dw_stride);
+    }
 }
 
 // dx of 256 rows and 128 numbers, summed over a share of the piece's vertices.
@@ -772,15 +861,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dx_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
                                                            T* __restrict__ dx, int64_t dx_stride) {
-    const int64_t live = a.header->n_live;
-    for (int64_t p = (int64_t)blockIdx.x * 4 + wave_id(); p < live; p += (int64_t)gridDim.x * 4) {
-        const float back = 1.f / a.header->scale;
-        const int64_t row = a.row_of[p];
-        for (int32_t e = lane_id(); e < a.d; e += kWave) {
-            float sum = 0.f;
-            for (int32_t s = 0; s < shares; ++s) sum += parts[((int64_t)s * a.n_pad + p) * a.dp + e];
-            dx[row * dx_stride + e] = (T)(sum * back);
-        }
+    const float back = 1.f / a.header->scale;
+    const int32_t across = (a.d + kJoinWidth - 1) / kJoinWidth;
+    const int64_t all = (int64_t)a.header->n_live * across;
+    for (int64_t i = (int64_t)blockIdx.x * 4 + wave_id(); i < all; i += (int64_t)gridDim.x * 4) {
+        const int64_t p = i / across;
+        const int32_t e = (int32_t)(i - p * across) * kJoinWidth + lane_id() * 4;
+        if (e < a.d) join_parts<T>(parts + p * a.dp, shares, a.n_pad * a.dp, back, e, a.d, dx + a.row_of[p] * dx_stride);
     }
 }
 
@@ -797,11 +884,12 @@ struct LossPlan {
     int32_t dp, groups, shares, dw_shares;
     bool few;                       // few rows, forward
     bool sweep;                     // rows short enough for nd_sweep.hip
+    bool kept;                      // the scores of all rows and vertices stay for the gradient
     // labels by vertex: the grouping's arrays, sums of their rows
     int64_t label_groups;
     SortPlan sort;
     size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group, o_label_parts;
-    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_parts, o_dw_parts, total;
+    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_scores, o_parts, o_dw_parts, total;
 };
 // 57,000 vertices, rows of 128 numbers in bf16: 8.3 us for one row, 1.5 us more for each, 19.4 for eight; nine rows the other
 // way 24.5 (fp32: 24.9 for eight, 48 for nine).
@@ -833,6 +921,14 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > 32768) piece_tiles = 32768;
     if (piece_tiles > v_tiles) piece_tiles = v_tiles;
+    // Scores are kept for the gradient where to write and read them takes less than to make them again: long rows, or so few
+    // scores that the last-level cache holds them.  With what comes before the products, kept and made again, us: 512 x
+    // 20,000 x 512 bf16 42 and 52, 4,096 x 20,000 x 512 239 and 253, 2,304 x 57,000 x 1,024 554 and 669, but 4,096 x 20,000
+    // x 320 206 and 187; fp32 4,096 x 4,096 x 128 73 and 97, 4,096 x 57,000 x 64 718 and 723.
+    const int64_t scores = p.n_pad * v_tiles * kTileM * 4;
+    p.kept = grad && !p.sweep && v_tiles <= 32768 && scores <= kKeptBytes &&
+             (p.dp >= (dtype == ND_F32 ? 64 : 512) || scores <= kCachedBytes);
+    if (p.kept) piece_tiles = v_tiles;
     p.piece = piece_tiles * kTileM;
     // the summed dimension is shared out where there are fewer tiles than two per compute unit; one more than that would
     // take as long as twice as many
@@ -896,6 +992,7 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     p.o_sum = take((size_t)p.groups * (size_t)p.n_pad * 4);
     if (grad) {
         p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
+        p.o_scores = p.kept && b < 4 ? take((size_t)p.piece * (size_t)p.n_pad * 4) : p.o_probs;
         p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
         p.o_dw_parts = p.dw_shares > 1 ? take((size_t)p.dw_shares * (size_t)p.piece * (size_t)p.dp * 4) : 0;
     }
@@ -1049,24 +1146,28 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         }
     const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
     if (c.n > 0) {
-        hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(p.n_pad / kTile * p.groups)), dim3(kThreads), 0, stream, a, ow, ox);
+        hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(p.n_pad / kTile * p.groups)), dim3(kThreads), 0, stream, a, ow, ox,
+                           p.kept ? (float*)(ws + p.o_scores) : nullptr);
         hipLaunchKernelGGL(loss_kernel<T>, wave_per(c.n), dim3(kThreads), 0, stream, a, rows, w, w_stride);
     }
     if (c.grad) {
         T* probs = (T*)(ws + p.o_probs);
         float* parts = (float*)(ws + p.o_parts);
         float* dw_parts = (float*)(ws + p.o_dw_parts);
-        const int64_t d_tiles = (p.dp + kTileN - 1) / kTileN;
+        const int64_t d_tiles = (p.dp + kTileN - 1) / kTileN, join_columns = (c.d + kJoinWidth - 1) / kJoinWidth;
         for (int64_t v = 0; v < c.V; v += p.piece) {
             const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTileM - 1) / kTileM;
             const Operand<T> op{probs, p.n_pad, tiles * kTileM, (int32_t)p.n_pad};
-            if (c.n > 0)
-                hipLaunchKernelGGL(probs_kernel<T>, dim3((unsigned)(p.n_pad / kTile * tiles)), dim3(kThreads), 0, stream, a, ow, ox, v, probs);
+            const dim3 all((unsigned)(p.n_pad / kTile * tiles));
+            if (c.n > 0 && p.kept)
+                hipLaunchKernelGGL(kept_kernel<T>, all, dim3(kThreads), 0, stream, a, (const float*)(ws + p.o_scores), probs);
+            else if (c.n > 0)
+                hipLaunchKernelGGL(probs_kernel<T>, all, dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)
                 hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)(tiles * d_tiles * p.dw_shares)), dim3(kThreads), 0, stream, a, op, ox, v,
                                    (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares);
             if (c.dw && p.dw_shares > 1)
-                hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
+                hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here * join_columns), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
                                    here, (T*)c.dw, c.dw_stride);
             if (c.dx && c.n > 0) {
                 const int64_t share = (tiles + p.shares - 1) / p.shares * kTileM;
@@ -1075,7 +1176,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
             }
         }
         if (c.dx && c.n > 0)
-            hipLaunchKernelGGL(dx_join_kernel<T>, wave_per(c.n), dim3(kThreads), 0, stream, a, parts, p.shares,
+            hipLaunchKernelGGL(dx_join_kernel<T>, wave_per(c.n * join_columns), dim3(kThreads), 0, stream, a, parts, p.shares,
                                (T*)c.dx, c.dx_stride);
     }
     ND_HIP_CHECK(hipGetLastError());

@@ -61,6 +61,15 @@ def test_vertices_in_several_pieces(kind):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,V,d,k", [(4100, 70000, 260, 3), (1030, 50001, 520, 1), (1500, 40001, 33, 64), (127, 3001, 1030, 4)])
+def test_scores_that_are_kept_and_made_again(n, V, d, k, kind):
+    """Long rows and few scores: kept between the two passes; many scores of shorter rows: made again, in pieces."""
+    x, w, labels, row_weight = (t.to(DEV) for t in _inputs(n, V, d, k, TYPES[kind], seed=d))
+    out = _run(x, w, labels, row_weight)
+    Loss(x, w, labels, row_weight).check(*out)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("d", [64, 72, 320])
 def test_rows_at_strides_and_odd_addresses(kind, d):
     n, V, k = 150, 333, 2
