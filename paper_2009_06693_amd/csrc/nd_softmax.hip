@@ -813,6 +813,7 @@ __device__ __forceinline__ void join_parts(const float* __restrict__ parts, int3
             if (e + q < d) to[e + q] = o.v[q];
     }
 }
+constexpr int kLeastShare = 64;  // of the summed dimension: a multiple of every Kind's step
 constexpr int kJoinWidth = kWave * 4;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
@@ -930,15 +931,17 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
              (p.dp >= (dtype == ND_F32 ? 64 : 512) || scores <= kCachedBytes);
     if (p.kept) piece_tiles = v_tiles;
     p.piece = piece_tiles * kTileM;
-    // the summed dimension is shared out where there are fewer tiles than two per compute unit; one more than that would
-    // take as long as twice as many
+    // The summed dimension is shared out where there are fewer tiles than two per compute unit; one more share than that
+    // would take as long as twice as many.  More than 16 shares cost more to join than the second workgroup of a compute
+    // unit gives (4,096 x 4,096 x 128 fp32: 16 and 32 shares both 55 us, and 7 and 12 to join), so beyond them it is one
+    // (1,000 x 20,000 x 100 fp32: dx 185 us with 16 shares, 60 with 64).
     auto shares = [](int64_t tiles, int64_t most) {
-        int64_t s = tiles < 512 ? 512 / tiles : 1;
-        s = s < 16 ? s : 16;
+        const int64_t two = tiles < 512 ? 512 / tiles : 1, one = tiles < 16 ? 256 / tiles : 16;
+        const int64_t s = two < one ? two : one;
         return (int32_t)(s < most ? s : most);
     };
-    p.shares = shares(p.n_pad / kTileM * ((p.dp + kTileN - 1) / kTileN), piece_tiles);
-    p.dw_shares = shares(piece_tiles * ((p.dp + kTileN - 1) / kTileN), p.blocks);
+    p.shares = shares(p.n_pad / kTileM * ((p.dp + kTileN - 1) / kTileN), p.piece / kLeastShare);
+    p.dw_shares = shares(piece_tiles * ((p.dp + kTileN - 1) / kTileN), p.blocks * kTile / kLeastShare);
     size_t o = sizeof(LossHeader);
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -1170,7 +1173,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
                 hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here * join_columns), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
                                    here, (T*)c.dw, c.dw_stride);
             if (c.dx && c.n > 0) {
-                const int64_t share = (tiles + p.shares - 1) / p.shares * kTileM;
+                const int64_t share = (tiles * kTileM / kLeastShare + p.shares - 1) / p.shares * kLeastShare;
                 hipLaunchKernelGGL(dx_kernel<T>, dim3((unsigned)(p.n_pad / kTileM * d_tiles * p.shares)), dim3(kThreads), 0, stream, a, op, ow,
                                    v, share, tiles * kTileM, (int)(v == 0), parts);
             }
