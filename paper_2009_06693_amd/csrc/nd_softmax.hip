@@ -22,8 +22,7 @@ constexpr int kThreads = 256;
 constexpr int kTile = 128;         // rows of a product's tile
 constexpr int kChunk = 16;         // bytes that a lane moves at once
 constexpr size_t kPieceBytes = (size_t)512 << 20;  // probabilities that lie in the workspace at a time, where scores are not kept
-constexpr int64_t kKeptBytes = (int64_t)4 << 30;    // scores that are kept at most,
-constexpr int64_t kCachedBytes = (int64_t)160 << 20;  // and where the cache holds them with what is made of them
+constexpr int64_t kKeptBytes = (int64_t)4 << 30;    // scores that are kept at most
 
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef short Short4 __attribute__((ext_vector_type(4)));
@@ -405,6 +404,25 @@ __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b
 __device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 128 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
 __device__ __forceinline__ int acc_col(int j) { return wave_id() % 2 * 64 + j * 32 + (lane_id() & 31); }
 
+// A wavefront's part of a tile, from the place of its lane's first number on: the `left` rows there are, and the columns
+// that are asked for; ADD: to what lies there.  One address that goes from row to row (with one for every number, dw of
+// 4,096 x 4,096 x 128 fp32 took 54 us, so 48).
+template <typename O, bool ADD>
+__device__ __forceinline__ void store_tile(const AccTile& acc, float factor, O* __restrict__ to, int64_t stride, int left,
+                                           bool first, bool second) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if (i * 32 + 8 * (r / 4) + r % 4 < left) {
+                if (first) to[0] = (O)((ADD ? to[0] : 0.f) + acc[i][0][r] * factor);
+                if (second) to[32] = (O)((ADD ? to[32] : 0.f) + acc[i][1][r] * factor);
+            }
+            to += (r % 4 == 3 ? 5 : 1) * stride;
+            asm volatile("" : "+v"(to));
+        }
+}
+
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -687,7 +705,10 @@ __device__ __forceinline__ void count_labels(const LossArgs& a, int64_t v0, int6
     __syncthreads();
 }
 
-// g (c p - count) of 256 vertices of the piece from v_first on and 128 rows, as [vertex][row].
+// What a vertex weighs in a row's gradient, as [vertex][row]: 256 vertices of the piece from v_first on, 128 rows.  In fp32
+// it is g (c p - count).  In 16 bits, to which it is rounded for the matrix instructions, it is g c p alone: one label can
+// outweigh all vertices, and the rounding of its count would be that of the whole gradient (fp16, relative to 64 bits, 3.2e-4
+// and without it 2.1e-4, which is the rounding of the result).  There the labels' rows are taken off afterwards, in 32 bits.
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
                                                          T* __restrict__ probs) {
@@ -698,33 +719,42 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
     AccTile acc;
     product<T, false, false>(w, x, v0, n0, 0, a.dp, lds, acc);
     uint8_t* counts = reinterpret_cast<uint8_t*>(lds);
-    count_labels(a, v0, n0, counts);
+    if constexpr (Kind<T>::kWide) count_labels(a, v0, n0, counts);
     const float scale = a.header->scale;
+    const int left = (int)(a.V - v0 < kTileM ? a.V - v0 : kTileM) - acc_row(0, 0);
+    float lse[2], c[2], g[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int col = acc_col(j);
-        const float lse = a.place_lse[n0 + col], c = a.count[n0 + col], g = a.weight[n0 + col] * scale;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = acc_row(i, r);
-                const float held = (float)counts[col * kCountPitch + row];
-                const float p = v0 + row < a.V && c > 0.f ? g * (c * exp_of(acc[i][j][r] - lse) - held) : 0.f;
-                probs[(m0 + row) * a.n_pad + n0 + col] = (T)p;
-            }
+        const int64_t place = n0 + acc_col(j);
+        lse[j] = a.place_lse[place];
+        c[j] = a.count[place];
+        g[j] = a.weight[place] * scale;
     }
+    T* to = probs + (m0 + acc_row(0, 0)) * a.n_pad + n0 + acc_col(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float held = Kind<T>::kWide ? (float)counts[acc_col(j) * kCountPitch + acc_row(i, r)] : 0.f;
+                const bool counts_here = i * 32 + 8 * (r / 4) + r % 4 < left && c[j] > 0.f;
+                to[j * 32] = (T)(counts_here ? g[j] * (c[j] * exp_of(acc[i][j][r] - lse[j]) - held) : 0.f);
+            }
+            to += (r % 4 == 3 ? 5 : 1) * a.n_pad;
+            asm volatile("" : "+v"(to));
+        }
 }
 
 // The same from scores that were kept; fp32: in their place.  A lane has four places.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float* scores, T* probs) {
-    __shared__ __align__(16) uint8_t counts[kTile * kCountPitch];
+    __shared__ __align__(16) uint8_t counts[Kind<T>::kWide ? kTile * kCountPitch : 16];
     constexpr int kLanes = kTile / 4, kRows = kThreads / kLanes, kAtOnce = 8;
     const int64_t id = tile_id(), blocks = a.n_pad / kTile;
     const int64_t n0 = id % blocks * kTile, v0 = id / blocks * kTileM;
     if (n0 >= (int64_t)a.header->n_live) return;
-    count_labels(a, v0, n0, counts);
+    if constexpr (Kind<T>::kWide) count_labels(a, v0, n0, counts);
     const float scale = a.header->scale;
     const int col = threadIdx.x % kLanes * 4, first = threadIdx.x / kLanes;
     float lse[4], c[4], g[4];
@@ -744,7 +774,7 @@ __global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float*
             Piece<T, 4> p;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float held = (float)counts[(col + e) * kCountPitch + row];
+                const float held = Kind<T>::kWide ? (float)counts[(col + e) * kCountPitch + row] : 0.f;
                 p.v[e] = (T)(v0 + row < a.V && c[e] > 0.f ? g[e] * (c[e] * exp_of(s[i].v[e] - lse[e]) - held) : 0.f);
             }
             store_piece<T, 4>(probs + (v0 + row) * a.n_pad + n0 + col, p);
@@ -752,12 +782,18 @@ __global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float*
     }
 }
 
+// The rows under every vertex that is a label, summed: by vertex, the row of the sums or -1 (null: nothing to take off).
+struct Labels {
+    const int32_t* row;
+    const float* sums;
+};
+
 // dw of 256 vertices of the piece and 128 numbers of their rows, over a share of the rows with labels: the result where
 // there is one share, else its part.
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
                                                       T* __restrict__ dw, int64_t dw_stride, float* __restrict__ parts,
-                                                      int64_t part_rows, int32_t shares) {
+                                                      int64_t part_rows, int32_t shares, Labels labels) {
     __shared__ __align__(16) char lds[kLdsBytes];
     // the tiles of one share, and of one tile of vertices, next to each other
     const int64_t id = tile_id(), d_tiles = (a.dp + kTileN - 1) / kTileN, v_tiles = gridDim.x / (d_tiles * shares);
@@ -766,28 +802,45 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
     const int64_t k0 = steps * share / shares * Kind<T>::kStep, k1 = steps * (share + 1) / shares * Kind<T>::kStep;
     AccTile acc;
     product<T, false, true>(probs, x, m0, d0, k0, k1, lds, acc);
-    const float back = 1.f / a.header->scale;
+    const float scale = a.header->scale, back = 1.f / scale;  // a power of two
+    if constexpr (!Kind<T>::kWide)
+        if (labels.row && shares == 1) {
+            // Few vertices are labels: the wavefront's 128 as bits, and what is taken off only where one is.  All of it before
+            // the first store, which a load's wait would wait for too.
+            int32_t sum[2];
+            uint64_t any[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t e = d0 + acc_col(j);
-        if (e >= a.d) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t m = m0 + acc_row(i, r);
-                if (v_first + m >= a.V) continue;
-                if (shares == 1)
-                    dw[(v_first + m) * dw_stride + e] = (T)(acc[i][j][r] * back);
-                else
-                    parts[(share * part_rows + m) * a.dp + e] = acc[i][j][r];
+            for (int h = 0; h < 2; ++h) {
+                const int64_t v = v_first + m0 + wave_id() / 2 * 128 + h * 64 + lane_id();
+                sum[h] = v < a.V ? labels.row[v] : -1;
+                any[h] = __ballot(sum[h] >= 0);
             }
-    }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = i * 32 + 8 * (r / 4) + r % 4;  // and 4 behind, the other half of the wavefront
+                    if (((any[at / 64] >> (at % 64)) & 0x11u) == 0) continue;
+                    const int32_t mine = __shfl(sum[at / 64], at % 64 + 4 * (lane_id() >> 5));
+                    if (mine >= 0)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (d0 + acc_col(j) < a.dp)
+                                acc[i][j][r] -= labels.sums[(int64_t)mine * a.dp + d0 + acc_col(j)] * scale;
+                }
+        }
+    const int64_t m = m0 + acc_row(0, 0), e = d0 + acc_col(0);
+    const int left = (int)(a.V - v_first - m < kTileM ? a.V - v_first - m : kTileM);  // rows from here on
+    if (shares == 1)
+        store_tile<T, false>(acc, back, dw + (v_first + m) * dw_stride + e, dw_stride, left, e < a.d, e + 32 < a.d);
+    else
+        store_tile<float, false>(acc, 1.f, parts + (share * part_rows + m) * a.dp + e, a.dp, left, e < a.d, e + 32 < a.d);
 }
+
 // Four numbers of a row, summed over the shares' parts: a wavefront has 256 numbers of one row, eight parts under way.
 template <typename T>
 __device__ __forceinline__ void join_parts(const float* __restrict__ parts, int32_t shares, int64_t share_size, float back,
-                                           int32_t e, int32_t d, T* __restrict__ to) {
+                                           const float (&less)[4], int32_t e, int32_t d, T* __restrict__ to) {
     constexpr int kAtOnce = 8;
     float sum[4] = {};
     for (int32_t s0 = 0; s0 < shares; s0 += kAtOnce) {
@@ -804,7 +857,7 @@ __device__ __forceinline__ void join_parts(const float* __restrict__ parts, int3
     }
     Piece<T, 4> o;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) o.v[q] = (T)(sum[q] * back);
+    for (int q = 0; q < 4; ++q) o.v[q] = (T)(sum[q] * back - less[q]);
     if (e + 4 <= d) {
         store_piece<T, 4>(to + e, o);
     } else {
@@ -818,13 +871,21 @@ constexpr int kJoinWidth = kWave * 4;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
                                                            int64_t part_rows, int64_t v_first, int64_t here, T* __restrict__ dw,
-                                                           int64_t dw_stride) {
+                                                           int64_t dw_stride, Labels labels) {
     const float back = 1.f / a.header->scale;
     const int32_t across = (a.d + kJoinWidth - 1) / kJoinWidth;
     for (int64_t i = (int64_t)blockIdx.x * 4 + wave_id(); i < here * across; i += (int64_t)gridDim.x * 4) {
         const int64_t m = i / across;
         const int32_t e = (int32_t)(i - m * across) * kJoinWidth + lane_id() * 4;
-        if (e < a.d) join_parts<T>(parts + m * a.dp, shares, part_rows * a.dp, back, e, a.d, dw + (v_first + m) * dw_stride);
+        if (e >= a.d) continue;
+        float less[4] = {};
+        const int32_t at = labels.row ? labels.row[v_first + m] : -1;
+        if (at >= 0) {
+            const Piece<float, 4> v = load_piece<float, 4>(labels.sums + (int64_t)at * a.dp + e);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) less[q] = v.v[q];
+        }
+        join_parts<T>(parts + m * a.dp, shares, part_rows * a.dp, back, less, e, a.d, dw + (v_first + m) * dw_stride);
     }
 }
 
@@ -845,30 +906,44 @@ __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads
     piece.rows -= v_first;
     AccTile acc;
     product<T, true, true>(probs, piece, n0, d0, k0, k1, lds, acc);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t e = d0 + acc_col(j);
-        if (e >= a.dp) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float* at = parts + (share * a.n_pad + n0 + acc_row(i, r)) * a.dp + e;
-                *at = first_piece ? acc[i][j][r] : *at + acc[i][j][r];
-            }
-    }
+    const int64_t e = d0 + acc_col(0);
+    float* to = parts + (share * a.n_pad + n0 + acc_row(0, 0)) * a.dp + e;
+    if (first_piece)
+        store_tile<float, false>(acc, 1.f, to, a.dp, kTileM, e < a.dp, e + 32 < a.dp);
+    else
+        store_tile<float, true>(acc, 1.f, to, a.dp, kTileM, e < a.dp, e + 32 < a.dp);
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dx_join_kernel(LossArgs a, const float* __restrict__ parts, int32_t shares,
-                                                           T* __restrict__ dx, int64_t dx_stride) {
+                                                           Operand<T> w, T* __restrict__ dx, int64_t dx_stride) {
     const float back = 1.f / a.header->scale;
     const int32_t across = (a.d + kJoinWidth - 1) / kJoinWidth;
     const int64_t all = (int64_t)a.header->n_live * across;
     for (int64_t i = (int64_t)blockIdx.x * 4 + wave_id(); i < all; i += (int64_t)gridDim.x * 4) {
         const int64_t p = i / across;
         const int32_t e = (int32_t)(i - p * across) * kJoinWidth + lane_id() * 4;
-        if (e < a.d) join_parts<T>(parts + p * a.dp, shares, a.n_pad * a.dp, back, e, a.d, dx + a.row_of[p] * dx_stride);
+        if (e >= a.d) continue;
+        float less[4] = {};
+        if constexpr (!Kind<T>::kWide) {  // the rows of the labels
+            constexpr int kAtOnce = 4;
+            for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
+                Piece<T, 4> v[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const int32_t label = j0 + j < a.k ? a.labels_of[p * a.k + j0 + j] : -1;
+                    v[j] = Piece<T, 4>{};
+                    if (label >= 0) v[j] = load_piece<T, 4>(w.base + label * w.stride + e);
+                }
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) less[q] += (float)v[j].v[q];
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) less[q] *= a.weight[p];
+        }
+        join_parts<T>(parts + p * a.dp, shares, a.n_pad * a.dp, back, less, e, a.d, dx + a.row_of[p] * dx_stride);
     }
 }
 
@@ -922,13 +997,12 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > 32768) piece_tiles = 32768;
     if (piece_tiles > v_tiles) piece_tiles = v_tiles;
-    // Scores are kept for the gradient where to write and read them takes less than to make them again: long rows, or so few
-    // scores that the last-level cache holds them.  With what comes before the products, kept and made again, us: 512 x
-    // 20,000 x 512 bf16 42 and 52, 4,096 x 20,000 x 512 239 and 253, 2,304 x 57,000 x 1,024 554 and 669, but 4,096 x 20,000
-    // x 320 206 and 187; fp32 4,096 x 4,096 x 128 73 and 97, 4,096 x 57,000 x 64 718 and 723.
-    const int64_t scores = p.n_pad * v_tiles * kTileM * 4;
-    p.kept = grad && !p.sweep && v_tiles <= 32768 && scores <= kKeptBytes &&
-             (p.dp >= (dtype == ND_F32 ? 64 : 512) || scores <= kCachedBytes);
+    // Scores are kept for the gradient where rows are long, so that to write and read them takes less than to make them again.
+    // Both ways with what comes before the products, us: 2,304 x 57,000 x 1,024 fp16 545 and 674, 512 x 20,000 x 512 bf16 42
+    // and 49, 4,096 x 20,000 x 512 232 and 236, but 2,000 x 20,000 x 320 104 and 93; fp32 4,096 x 4,096 x 128 72 and 94,
+    // 4,096 x 57,000 x 64 713 and 709.
+    p.kept = grad && !p.sweep && v_tiles <= 32768 && p.n_pad * v_tiles * kTileM * 4 <= kKeptBytes &&
+             p.dp >= (dtype == ND_F32 ? 128 : 512);
     if (p.kept) piece_tiles = v_tiles;
     p.piece = piece_tiles * kTileM;
     // The summed dimension is shared out where there are fewer tiles than two per compute unit; one more share than that
@@ -958,6 +1032,25 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     p.o_labels = take((size_t)p.n_pad * (size_t)k * 4);
     p.o_rows = take((size_t)p.n_pad * (size_t)p.dp * (size_t)b);
     p.o_w = take((size_t)V * (size_t)p.dp * (size_t)b);
+    auto take_labels = [&] {
+        const size_t slots = (size_t)n * (size_t)k, some = slots > 0 ? slots : 1;
+        const size_t tiles = (size_t)group_sum_tiles((int64_t)slots, p.dp, dtype);
+        p.label_groups = (int64_t)slots < V ? (int64_t)slots : V;
+        p.sort = make_sort_plan((int64_t)slots, V);
+        p.o_ctl = take(sizeof(StepCtl));
+        for (int i = 0; i < 2; ++i) {
+            p.o_keys[i] = take(some * 4);
+            p.o_vals[i] = take(some * 4);
+        }
+        p.o_hist = take(sort_hist_bytes(p.sort));
+        p.o_scratch = take(seg_scratch_bytes((int64_t)slots));
+        p.o_gkey = take(some * 4);
+        p.o_gstart = take((some + 1) * 4);
+        p.o_label_row = take((size_t)V * 4);
+        p.o_label_sums = take((size_t)p.label_groups * (size_t)p.dp * 4);
+        p.o_tile_group = take(tiles * 4);
+        p.o_label_parts = take(tiles * 2 * (size_t)p.dp * 4);
+    };
     if (p.sweep) {
         // the sweeps run one after the other and share the segments' memory
         size_t held = 0, sums = 0;
@@ -969,31 +1062,14 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
         p.o_max = take(held * 4);
         p.o_sum = take(held * 4);
         p.o_parts = take(sums * (size_t)p.dp * 4);
-        if (grad) {
-            const size_t slots = (size_t)n * (size_t)k, some = slots > 0 ? slots : 1;
-            const size_t tiles = (size_t)group_sum_tiles((int64_t)slots, p.dp, dtype);
-            p.label_groups = (int64_t)slots < V ? (int64_t)slots : V;
-            p.sort = make_sort_plan((int64_t)slots, V);
-            p.o_ctl = take(sizeof(StepCtl));
-            for (int i = 0; i < 2; ++i) {
-                p.o_keys[i] = take(some * 4);
-                p.o_vals[i] = take(some * 4);
-            }
-            p.o_hist = take(sort_hist_bytes(p.sort));
-            p.o_scratch = take(seg_scratch_bytes((int64_t)slots));
-            p.o_gkey = take(some * 4);
-            p.o_gstart = take((some + 1) * 4);
-            p.o_label_row = take((size_t)V * 4);
-            p.o_label_sums = take((size_t)p.label_groups * (size_t)p.dp * 4);
-            p.o_tile_group = take(tiles * 4);
-            p.o_label_parts = take(tiles * 2 * (size_t)p.dp * 4);
-        }
+        if (grad) take_labels();
         p.total = o;
         return p;
     }
     p.o_max = take((size_t)p.groups * (size_t)p.n_pad * 4);
     p.o_sum = take((size_t)p.groups * (size_t)p.n_pad * 4);
     if (grad) {
+        if (dtype != ND_F32) take_labels();
         p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
         p.o_scores = p.kept && b < 4 ? take((size_t)p.piece * (size_t)p.n_pad * 4) : p.o_probs;
         p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
@@ -1157,6 +1233,14 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         T* probs = (T*)(ws + p.o_probs);
         float* parts = (float*)(ws + p.o_parts);
         float* dw_parts = (float*)(ws + p.o_dw_parts);
+        Labels labels{};
+        if constexpr (sizeof(T) == 2)
+            if (c.dw && c.n > 0) {
+                SweepParts sums{};
+                const int rc = sum_labels<T>(a, p, ws, rows, &sums, stream);
+                if (rc != ND_OK) return rc;
+                labels = {sums.label_row, sums.label_sums};
+            }
         const int64_t d_tiles = (p.dp + kTileN - 1) / kTileN, join_columns = (c.d + kJoinWidth - 1) / kJoinWidth;
         for (int64_t v = 0; v < c.V; v += p.piece) {
             const int64_t here = c.V - v < p.piece ? c.V - v : p.piece, tiles = (here + kTileM - 1) / kTileM;
@@ -1168,10 +1252,10 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
                 hipLaunchKernelGGL(probs_kernel<T>, all, dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)
                 hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)(tiles * d_tiles * p.dw_shares)), dim3(kThreads), 0, stream, a, op, ox, v,
-                                   (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares);
+                                   (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares, labels);
             if (c.dw && p.dw_shares > 1)
                 hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here * join_columns), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
-                                   here, (T*)c.dw, c.dw_stride);
+                                   here, (T*)c.dw, c.dw_stride, labels);
             if (c.dx && c.n > 0) {
                 const int64_t share = (tiles * kTileM / kLeastShare + p.shares - 1) / p.shares * kLeastShare;
                 hipLaunchKernelGGL(dx_kernel<T>, dim3((unsigned)(p.n_pad / kTileM * d_tiles * p.shares)), dim3(kThreads), 0, stream, a, op, ow,
@@ -1180,7 +1264,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         }
         if (c.dx && c.n > 0)
             hipLaunchKernelGGL(dx_join_kernel<T>, wave_per(c.n * join_columns), dim3(kThreads), 0, stream, a, parts, p.shares,
-                               (T*)c.dx, c.dx_stride);
+                               ow, (T*)c.dx, c.dx_stride);
     }
     ND_HIP_CHECK(hipGetLastError());
     return ND_OK;

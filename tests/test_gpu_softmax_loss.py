@@ -4,7 +4,7 @@ import torch
 
 from paper_2009_06693_amd import binding as B
 
-from rows_util import TYPES, Loss
+from rows_util import TYPES, U32, Loss, assert_within, half_step, rounded
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -60,10 +60,28 @@ def test_vertices_in_several_pieces(kind):
     Loss(x, w, labels, row_weight).check(*out)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [128, 300, 520])
+def test_labels_are_not_rounded_with_the_vertices(kind, d):
+    """Equal scores: every vertex weighs 1 / V and the label almost 1.  What is rounded to 16 bits before the products is a
+    vertex's weight, off by u of itself, so that dx is off by u times the mean row's size next to its own rounding."""
+    n, V, dtype = 70, 2500, TYPES[kind]
+    g = torch.Generator().manual_seed(d)
+    w = torch.randn(V, d, generator=g).to(dtype)
+    labels = torch.randint(0, V, (n, 1), generator=g).int()
+    row_weight = torch.rand(n, generator=g) + 0.1
+    _, _, dx, _ = _run(torch.zeros(n, d, dtype=dtype, device=DEV), w.to(DEV), labels.to(DEV), row_weight.to(DEV))
+    wd, gd = w.double(), row_weight.double()[:, None]
+    want = gd * (wd.mean(0) - wd[labels[:, 0].long()])
+    size = gd * wd.abs().mean(0)
+    off = half_step(dtype) * size + (V + 16) * U32 * (size + want.abs())
+    assert_within(dx, want, rounded(want, off, dtype), "dx")
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("n,V,d,k", [(4100, 70000, 260, 3), (1030, 50001, 520, 1), (1500, 40001, 33, 64), (127, 3001, 1030, 4)])
 def test_scores_that_are_kept_and_made_again(n, V, d, k, kind):
-    """Long rows and few scores: kept between the two passes; many scores of shorter rows: made again, in pieces."""
+    """Long rows: scores are kept between the two passes; shorter ones: made again, here in pieces."""
     x, w, labels, row_weight = (t.to(DEV) for t in _inputs(n, V, d, k, TYPES[kind], seed=d))
     out = _run(x, w, labels, row_weight)
     Loss(x, w, labels, row_weight).check(*out)
