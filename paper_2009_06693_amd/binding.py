@@ -474,6 +474,8 @@ def nd_softmax_loss_grad(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor,
 
 
 def nd_softmax_loss_status(workspace: torch.Tensor, stream=None):
+    if not workspace.is_cuda or workspace.numel() * workspace.element_size() < 4:
+        raise TypeError("workspace must be a CUDA tensor that a call has used")
     _check(lib().nd_softmax_loss_status(workspace.data_ptr(), _stream_ptr(stream)))
 
 

@@ -736,7 +736,7 @@ int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n,
         set_error("%lld rows for %lld groups", (long long)out_rows, (long long)n_groups);
         return ND_ERR_BAD_ARGUMENT;
     }
-    if (out_rows >= (1ll << 31) || n_groups >= (1ll << 31)) {
+    if (out_rows >= (1ll << 31) || n_groups >= (1ll << 31) || out_rows + n_groups >= (1ll << 32) - 1024) {
         set_error("fewer than 2^31 rows and groups");
         return ND_ERR_TOO_LARGE;
     }

@@ -41,13 +41,19 @@ __device__ __forceinline__ int32_t labels_of_row(const LossArgs& a, int64_t row,
     return c;
 }
 
+// What the scale goes by: an infinite weight or one that is no number must not take the others' gradients with it.
+__device__ __forceinline__ float weight_size(const LossArgs& a, int64_t row) {
+    const float w = a.row_weight ? fabsf(a.row_weight[row]) : 1.f;
+    return w <= FLT_MAX ? w : 0.f;
+}
+
 __global__ __launch_bounds__(kTile) void count_kernel(LossArgs a) {
     __shared__ uint32_t s_live[2], s_bad[2];
     __shared__ float s_weight[2];
     const int64_t row = (int64_t)blockIdx.x * kTile + threadIdx.x;
     bool bad = false;
     const bool live = row < a.n && labels_of_row(a, row, &bad) > 0;
-    float w = live ? (a.row_weight ? fabsf(a.row_weight[row]) : 1.f) : 0.f;
+    float w = live ? weight_size(a, row) : 0.f;
     for (int s = 32; s > 0; s >>= 1) w = fmaxf(w, __shfl_xor(w, s));
     const uint64_t lives = __ballot(live), bads = __ballot(bad);
     if (lane_id() == 0) {
@@ -76,7 +82,7 @@ __global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks
     if (blocks == 1) {  // nothing was counted
         all = c > 0;
         bad_any = bad;
-        top = c > 0 ? (a.row_weight ? fabsf(a.row_weight[row]) : 1.f) : 0.f;
+        top = c > 0 ? weight_size(a, row) : 0.f;
     } else {
         for (int32_t b = threadIdx.x; b < blocks; b += kTile) {
             const uint32_t l = a.block_live[b];
@@ -109,7 +115,7 @@ __global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks
         a.header->n_live = all;
         // fp16 holds 2^-24 to 65,504: the largest product of a weight and a count of labels becomes at most 2^15
         float scale = 1.f;
-        if (std::is_same<T, f16_t>::value && top > 0.f && top < FLT_MAX)
+        if (std::is_same<T, f16_t>::value && top > 0.f)
             scale = exp2f(fminf(fmaxf(floorf(log2f(32768.f / (float)a.k) - log2f(top)), -60.f), 60.f));
         a.header->scale = scale;
     }
@@ -611,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(LossArgs a, const T* __re
                     __builtin_memcpy(&f, __builtin_assume_aligned(rows + n * a.d + at, VEC >= 4 ? 16 : 4), sizeof(f));
                 else
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) f.v[e] = rows[n * a.d + at + e];
+                    for (int e = 0; e < VEC; ++e) f.v[e] = e < skip ? 0.f : rows[n * a.d + at + e];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
 #pragma unroll

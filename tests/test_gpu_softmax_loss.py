@@ -177,6 +177,22 @@ def test_weights_of_rows():
         Loss(x, w, labels, row_weight).check(*_run(*args, row_weight.to(DEV)), what=f"{kind} mixed")
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("d", [64, 300])
+@pytest.mark.parametrize("n", [60, 300])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_a_weight_that_is_not_finite_leaves_other_rows_alone(kind, d, n, value):
+    x, w, labels, row_weight = (t.to(DEV) for t in _inputs(n, 700, d, 2, TYPES[kind], seed=n))
+    labels[5, 0] = 3
+    row_weight[:] = 1e-4
+    want = _run(x, w, labels, row_weight)[2].clone()
+    row_weight[5] = value
+    got = _run(x, w, labels, row_weight)[2]
+    others = torch.arange(n, device=DEV) != 5
+    assert torch.equal(got[others], want[others])
+    assert not bool(got[5].isfinite().any())
+
+
 def test_only_the_gradients_that_are_asked_for():
     x, w, labels, row_weight = (t.to(DEV) for t in _inputs(200, 700, 128, 2, torch.bfloat16, seed=19))
     loss, lse, dx, dw = _run(x, w, labels, row_weight)
