@@ -409,9 +409,9 @@ int nd_samples_pack(const int32_t* const* step_out_dev, int32_t num_steps, const
  * From samples to training: rows of features, in device memory, one row of d numbers per vertex, sample or slot.
  * `dtype` is an nd_dtype and the same for all rows of a call; a row's numbers lie next to each other, rows a fixed
  * number of elements (`*_stride`, at least d) apart, at any address that is a multiple of the type's size.  Sums are
- * held in 32-bit floats and rounded once, to nearest, ties to even.  All calls are asynchronous on hip_stream, allocate nothing, never
- * wait and can be captured into a graph; equal inputs give equal outputs, bit for bit.  Pointers belong to the current
- * device.  Outputs must not overlap inputs.
+ * held in 32-bit floats and rounded once, to nearest, ties to even.  All calls are asynchronous on hip_stream, allocate
+ * nothing, never wait and can be captured into a graph; equal inputs give equal outputs, bit for bit.  Pointers belong to
+ * the current device.  Outputs must not overlap inputs.
  */
 typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
 #define ND_MAX_ROW 8192     /* numbers in a row */
@@ -439,9 +439,12 @@ typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
  *   workspace_dev    nd_softmax_loss_workspace_bytes bytes, 256-byte aligned, owned by the caller (grad: for
  *                    nd_softmax_loss_grad); calls that overlap in time need one each
  *
- * Logits never exist as a whole: at most a piece of vertices at a time, in the workspace or in registers.  Their
- * probabilities are rounded to the type of the rows before they are multiplied by rows.  A label of V
- * or more counts as NULL and is recorded: nd_softmax_loss_status waits for the stream and returns ND_ERR_BAD_ROOT then.
+ * Up to 256 16-bit numbers a row no score leaves the registers.  Of longer rows, and in fp32, scores and what is made of
+ * them lie in the workspace: at most 512 MB of probabilities at a time, or up to 4 GB of scores where rows are so long that
+ * they are cheaper to keep than to make twice.  Before they are multiplied by rows, probabilities are rounded to the type of
+ * the rows; what labels weigh is not (fp32: both stay in fp32).  fp16: row_weight p is held in steps no finer than 2^-39 k of
+ * the largest finite row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status waits for the
+ * stream and returns ND_ERR_BAD_ROOT then.  Infinities and NaN in a row of x stay in that row's loss, lse and dx.
  * Limits: n < 2^30, V < 2^31, d <= ND_MAX_ROW, k <= ND_MAX_LABELS, n * k < 2^31.  Errors: ND_ERR_NULL_POINTER,
  * ND_ERR_BAD_ARGUMENT, ND_ERR_TOO_LARGE, ND_ERR_WORKSPACE, ND_ERR_HIP.
  */
@@ -471,10 +474,12 @@ int nd_softmax_loss_status(const void* workspace_dev, void* hip_stream);
  *                       whatever their weight; index = positions brings rows in group order back, index = sampled
  *                       vertices sums their rows out of a table (a GraphSAGE aggregator; m = 1: a look-up)
  * nd_rows_weight_grad   dweights[r m + j] = dy_r . z_index[r m + j], 0 where nd_rows_to_samples skips
- * nd_rows_group_sum     out_u = sum over the pairs p of group u of weights[q] x_(q div m), q = sorted_slots[p], in the
- *                       order of the pairs within pieces of equal size; the gradient of rows that several slots read.  group_row_dev NULL: out has
- *                       n_groups rows; otherwise (device, nd_group_by_transit's group_transit: ascending) group u's sum is row
- *                       group_row[u] of out, and the other of its out_rows rows are 0
+ * nd_rows_group_sum     out_u = sum over the pairs p of group u, those from group_start[u] to group_start[u + 1]
+ *                       (n_groups + 1 offsets that do not descend, as nd_group_by_transit gives them), of weights[q]
+ *                       x_(q div m), q = sorted_slots[p]: the gradient of rows that several slots read.  group_row_dev
+ *                       NULL: out has n_groups rows; otherwise (device, nd_group_by_transit's group_transit: ascending,
+ *                       none twice) group u's sum is row group_row[u] of out, and the others of its out_rows rows are 0.
+ *                       A group without pairs is a row of zeros.  Fewer than 2^31 groups and rows of out
  *
  * Gradients: of nd_rows_by_transit by x, nd_rows_to_samples of the incoming gradient over the positions; of
  * nd_rows_to_samples by z, nd_rows_by_transit of the incoming gradient where index = positions, nd_rows_group_sum of it

@@ -211,7 +211,8 @@ __device__ __forceinline__ void fold(float (&dot)[N], int lane, int* s, int* fir
 }
 
 // 2^log_lanes lanes of a wavefront share the dot products of one row with SLOTS of its slots' rows, whose pieces are under
-// way together (four: 231 us for 233,000 rows of 25 slots x 128 bf16; eight 288).  In the first steps of the sum over the lanes, half of them go on with half of the products each.
+// way together (four: 231 us for 233,000 rows of 25 slots x 128 bf16; eight 288).  In the first steps of the sum over the
+// lanes, half of them go on with half of the products each.
 template <typename T, int VEC, int SLOTS>
 __global__ __launch_bounds__(kThreads) void weight_grad_kernel(const T* __restrict__ dy, int64_t dy_stride,
                                                                const T* __restrict__ z, int64_t z_stride, uint32_t n_z,
@@ -418,7 +419,8 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
 }
 
 template <typename T, int VEC>
-__device__ __forceinline__ void store_group(const GroupSum& g, int64_t u, int32_t at, const float (&sum)[VEC], T* __restrict__ out) {
+__device__ __forceinline__ void store_group(const GroupSum& g, int64_t u, int32_t at, const float (&sum)[VEC],
+                                            T* __restrict__ out) {
     const int64_t r = row_of_group(g, u);
     if (r >= 0) store_sum<T, VEC>(out + r * g.out_stride + at, sum);
 }
@@ -523,8 +525,8 @@ int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t
     const int64_t tile_blocks = sums ? (g.n_groups + kThreads - 1) / kThreads : 0;
     const int64_t clear_blocks = g.group_row ? (g.out_rows + kThreads - 1) / kThreads : 0;
     if (tile_blocks + clear_blocks > 0)
-        hipLaunchKernelGGL((group_tiles_kernel<O, VEC>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(kThreads), 0, stream, d,
-                           t, g, tile_blocks, out);
+        hipLaunchKernelGGL((group_tiles_kernel<O, VEC>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(kThreads), 0, stream,
+                           d, t, g, tile_blocks, out);
     if (sums)
         hipLaunchKernelGGL((group_sum_kernel<T, O, VEC, BY_ROW>), dim3(workgroups((tiles + t.rows - 1) / t.rows), deal_columns(t)),
                            dim3(deal_threads(t)), 0, stream, x, x_stride, d, t, make_fastdiv((uint32_t)m), (uint32_t)(n * m),

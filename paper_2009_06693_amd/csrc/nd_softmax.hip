@@ -282,7 +282,8 @@ struct Mover {
                 v[SET][i] = *reinterpret_cast<const Word4*>(at[i] + k);
             } else {
                 const uint32_t r = ((uint32_t)(i * kThreads) + threadIdx.x) / kPieces;
-                v[SET][i] = *reinterpret_cast<const Word4*>(across + ((uint64_t)(r < left ? r : left - 1u) * (uint32_t)o.stride + (uint32_t)column[i]));
+                v[SET][i] = *reinterpret_cast<const Word4*>(
+                    across + ((uint64_t)(r < left ? r : left - 1u) * (uint32_t)o.stride + (uint32_t)column[i]));
             }
         }
     }
@@ -407,7 +408,9 @@ __device__ __forceinline__ void product(const Operand<T>& a, const Operand<T>& b
     if (k < k1) step(k, std::integral_constant<int, 0>());
     __syncthreads();
 }
-__device__ __forceinline__ int acc_row(int i, int r) { return wave_id() / 2 * 128 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4; }
+__device__ __forceinline__ int acc_row(int i, int r) {
+    return wave_id() / 2 * 128 + i * 32 + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4;
+}
 __device__ __forceinline__ int acc_col(int j) { return wave_id() % 2 * 64 + j * 32 + (lane_id() & 31); }
 
 // A wavefront's part of a tile, from the place of its lane's first number on: the `left` rows there are, and the columns
@@ -443,7 +446,8 @@ __device__ __forceinline__ int64_t tile_id() {
 // A workgroup takes 128 rows and every groups-th tile of 256 vertices; a lane keeps maximum and sum of its two columns.
 // scores (may be null): the products themselves, as [vertex][row].
 template <typename T>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads)
+void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x,
                                                          float* __restrict__ scores) {
     __shared__ __align__(16) char lds[kLdsBytes];
     const int64_t id = tile_id(), blocks = a.n_pad / kTile, group = id / blocks, n0 = id % blocks * kTile;
@@ -565,8 +569,6 @@ __device__ __forceinline__ float lane_sum(float v, int log_lanes) {
     if (log_lanes > 1) v += __uint_as_float(dpp_moved<0x4E, 0xf>(__float_as_uint(v)));   // 2, 3, 0, 1
     if (log_lanes > 2) v += __uint_as_float(dpp_moved<0x141, 0xf>(__float_as_uint(v)));  // eight lanes mirrored
     if (log_lanes > 3) v += __uint_as_float(dpp_moved<0x140, 0xf>(__float_as_uint(v)));  // sixteen
-    if (log_lanes > 4) v += __shfl_xor(v, 16);
-    if (log_lanes > 5) v += __shfl_xor(v, 32);
     return v;
 }
 __device__ __forceinline__ void join_sums(float& top, float& sum, float top2, float sum2) {
@@ -578,16 +580,19 @@ __device__ __forceinline__ void join_sums(float& top, float& sum, float top2, fl
 template <typename T, int VEC, int N>
 __global__ __launch_bounds__(kThreads) void few_kernel(LossArgs a, const T* __restrict__ x, int64_t x_stride,
                                                        const T* __restrict__ w, int64_t w_stride, int log_lanes) {
-    extern __shared__ __align__(16) float rows[];  // [N][d]
+    extern __shared__ __align__(16) float rows[];  // [N][pitch]: a last piece that reaches back has zeros for what it shares
     __shared__ float s_top[4][N], s_sum[4][N];
-    for (int32_t e = threadIdx.x; e < N * a.d; e += kThreads) {
-        const int32_t n = e / a.d;
-        rows[e] = n < (int32_t)a.n ? (float)x[n * x_stride + (e - n * a.d)] : 0.f;
+    const int32_t pitch = (a.d + VEC - 1) / VEC * VEC, back = pitch - a.d, shared_from = pitch - VEC;
+    for (int32_t i = threadIdx.x; i < N * pitch; i += kThreads) {
+        const int32_t n = i / pitch, e = i - n * pitch;
+        const bool held = n < (int32_t)a.n && (e < shared_from || e - shared_from >= back);
+        rows[i] = held ? (float)x[n * x_stride + (e < shared_from ? e : e - back)] : 0.f;
     }
     __syncthreads();
     const int lanes = 1 << log_lanes, lane = lane_id() & (lanes - 1), per_wave = kWave >> log_lanes;
     const int64_t per_group = 4 * per_wave * kFewAtOnce;
-    const bool whole = a.d % VEC == 0;
+    const bool upper = lane & (lanes >> 1), odd = lane & (lanes >> 2);
+    const int mine = (upper ? 2 : 0) + (odd ? 1 : 0);  // of the vertices under way
     float top[N], sum[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -605,7 +610,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(LossArgs a, const T* __re
                 const int64_t row = v + u * per_wave < a.V ? v + u * per_wave : a.V - 1;
                 p[u] = load_piece<T, VEC>(w + row * w_stride + at);
             }
-            if (!whole)  // what another lane has is counted there
+            if (skip > 0)  // what another lane has is counted there
 #pragma unroll
                 for (int u = 0; u < kFewAtOnce; ++u)
 #pragma unroll
@@ -613,34 +618,31 @@ __global__ __launch_bounds__(kThreads) void few_kernel(LossArgs a, const T* __re
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 Piece<float, VEC> f;
-                if (whole)
-                    __builtin_memcpy(&f, __builtin_assume_aligned(rows + n * a.d + at, VEC >= 4 ? 16 : 4), sizeof(f));
-                else
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) f.v[e] = e < skip ? 0.f : rows[n * a.d + at + e];
+                __builtin_memcpy(&f, __builtin_assume_aligned(rows + n * pitch + c, VEC >= 4 ? 16 : 4), sizeof(f));
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
 #pragma unroll
                     for (int u = 0; u < kFewAtOnce; ++u) dot[u][n] = fmaf((float)p[u].v[e], f.v[e], dot[u][n]);
             }
         }
+        // each quarter of the lanes goes on with one of the four vertices, so that an exponential is taken four times less
+        // often and fewer sums cross the lanes
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            float t = top[n];
+            float half[2];
 #pragma unroll
-            for (int u = 0; u < kFewAtOnce; ++u) {
-                dot[u][n] = v + u * per_wave < a.V ? lane_sum(dot[u][n], log_lanes) : -INFINITY;
-                t = fmaxf(t, dot[u][n]);
+            for (int u = 0; u < 2; ++u) {
+                const float keep = upper ? dot[2 + u][n] : dot[u][n], give = upper ? dot[u][n] : dot[2 + u][n];
+                half[u] = keep + __shfl_xor(give, lanes >> 1);
             }
-            sum[n] *= exp_of(top[n] - t);
-#pragma unroll
-            for (int u = 0; u < kFewAtOnce; ++u) sum[n] += exp_of(dot[u][n] - t);
-            top[n] = t;
+            float score = (odd ? half[1] : half[0]) + __shfl_xor(odd ? half[0] : half[1], lanes >> 2);
+            score = lane_sum(score, log_lanes - 2);
+            if (v + mine * per_wave < a.V) join_sums(top[n], sum[n], score, 1.f);
         }
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        for (int s = 32; s >= lanes; s >>= 1) join_sums(top[n], sum[n], __shfl_xor(top[n], s), __shfl_xor(sum[n], s));
+        for (int s = 32; s >= lanes >> 2; s >>= 1) join_sums(top[n], sum[n], __shfl_xor(top[n], s), __shfl_xor(sum[n], s));
         if (lane_id() == 0) {
             s_top[wave_id()][n] = top[n];
             s_sum[wave_id()][n] = sum[n];
@@ -716,7 +718,8 @@ __device__ __forceinline__ void count_labels(const LossArgs& a, int64_t v0, int6
 // outweigh all vertices, and the rounding of its count would be that of the whole gradient (fp16, relative to 64 bits, 3.2e-4
 // and without it 2.1e-4, which is the rounding of the result).  There the labels' rows are taken off afterwards, in 32 bits.
 template <typename T>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads)
+void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
                                                          T* __restrict__ probs) {
     __shared__ __align__(16) char lds[kLdsBytes];
     const int64_t id = tile_id(), blocks = a.n_pad / kTile;
@@ -797,7 +800,8 @@ struct Labels {
 // dw of 256 vertices of the piece and 128 numbers of their rows, over a share of the rows with labels: the result where
 // there is one share, else its part.
 template <typename T>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads)
+void dw_kernel(LossArgs a, Operand<T> probs, Operand<T> x, int64_t v_first,
                                                       T* __restrict__ dw, int64_t dw_stride, float* __restrict__ parts,
                                                       int64_t part_rows, int32_t shares, Labels labels) {
     __shared__ __align__(16) char lds[kLdsBytes];
@@ -897,7 +901,8 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, const flo
 
 // dx of 256 rows and 128 numbers, summed over a share of the piece's vertices.
 template <typename T>
-__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads) void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
+__global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads)
+void dx_kernel(LossArgs a, Operand<T> probs, Operand<T> w, int64_t v_first,
                                                       int64_t v_share, int64_t v_end, int first_piece,
                                                       float* __restrict__ parts) {
     __shared__ __align__(16) char lds[kLdsBytes];
@@ -970,11 +975,13 @@ struct LossPlan {
     // labels by vertex: the grouping's arrays, sums of their rows
     int64_t label_groups;
     SortPlan sort;
-    size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group, o_label_parts;
-    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_scores, o_parts, o_dw_parts, total;
+    size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group,
+        o_label_parts;
+    size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_scores,
+        o_parts, o_dw_parts, total;
 };
-// 57,000 vertices, rows of 128 numbers in bf16: 8.3 us for one row, 1.5 us more for each, 19.4 for eight; nine rows the other
-// way 24.5 (fp32: 24.9 for eight, 48 for nine).
+// 57,000 vertices, rows of 128 numbers in bf16: 8.4 us for one row, 17.8 for eight; nine rows the other way 24.5 (fp32: 19 for
+// eight, 48 for nine; rows of 1,000 in bf16: 49 and 87).
 bool few_rows(int64_t n, int32_t d, bool grad) {
     if (grad || n < 1 || n > kFewRows) return false;
     int rows = 1;
@@ -1125,9 +1132,10 @@ int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, Sw
                         1, nullptr, &keys, &vals, stream);
     if (rc == ND_OK) rc = build_groups(keys, slots, ctl, g_key, g_start, (uint32_t*)(ws + p.o_scratch), nullptr, 0, stream);
     if (rc != ND_OK) return rc;
-    hipLaunchKernelGGL(label_clear_kernel, dim3((unsigned)((a.V + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, label_row, a.V);
-    hipLaunchKernelGGL(label_rows_kernel, dim3((unsigned)((p.label_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, ctl,
-                       g_key, p.label_groups, label_row);
+    hipLaunchKernelGGL(label_clear_kernel, dim3((unsigned)((a.V + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream,
+                       label_row, a.V);
+    hipLaunchKernelGGL(label_rows_kernel, dim3((unsigned)((p.label_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                       stream, ctl, g_key, p.label_groups, label_row);
     ND_HIP_CHECK(hipGetLastError());
     GroupSum g{};
     g.slots = vals;
@@ -1145,11 +1153,12 @@ int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, Sw
 
 template <typename T, int VEC, int N>
 void launch_few(LossArgs& a, const LossCall& c, hipStream_t stream) {
-    int log_lanes = 0;
+    int log_lanes = 2;  // four lanes at least, one for each vertex under way
     while (log_lanes < 6 && (VEC << log_lanes) < c.d) ++log_lanes;
     const int64_t per = 4 * (kWave >> log_lanes) * kFewAtOnce, groups = (c.V + per - 1) / per;
     a.groups = (int32_t)(groups < kFewGroups ? groups : kFewGroups);
-    hipLaunchKernelGGL((few_kernel<T, VEC, N>), dim3((unsigned)a.groups), dim3(kThreads), (size_t)N * c.d * 4, stream, a,
+    hipLaunchKernelGGL((few_kernel<T, VEC, N>), dim3((unsigned)a.groups), dim3(kThreads),
+                       (size_t)N * ((c.d + VEC - 1) / VEC * VEC) * 4, stream, a,
                        (const T*)c.x, c.x_stride, (const T*)c.w, c.w_stride, log_lanes);
     hipLaunchKernelGGL(few_finish_kernel<T>, dim3((unsigned)c.n), dim3(kThreads), 0, stream, a, (const T*)c.x, c.x_stride,
                        (const T*)c.w, c.w_stride, (int32_t)N);
@@ -1208,7 +1217,8 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     const T* w = (const T*)c.w;
     int64_t w_stride = c.w_stride;
     // a stride beyond 2^24 numbers would leave 32 bits within a sweep's unit
-    const bool as_it_is = c.d == p.dp && w_stride < (1 << 24) && w_stride * (int64_t)sizeof(T) % kChunk == 0 && (uintptr_t)w % kChunk == 0;
+    const bool as_it_is = c.d == p.dp && w_stride < (1 << 24) && w_stride * (int64_t)sizeof(T) % kChunk == 0 &&
+                          (uintptr_t)w % kChunk == 0;
     if (!as_it_is) {
         T* padded = (T*)(ws + p.o_w);
         hipLaunchKernelGGL(pad_kernel<T>, spread_grid(spread, c.V), dim3(kThreads), 0, stream, w, w_stride, c.V, c.d, p.dp,
@@ -1226,7 +1236,8 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
                 if (rc == ND_OK) rc = sweep_finish<T>(mode, a, rows, w, w_stride, parts, (T*)c.dx, c.dx_stride, stream);
             }
             if (rc == ND_OK && c.grad && c.dw && c.n > 0) rc = sum_labels<T>(a, p, ws, rows, &parts, stream);
-            if (rc == ND_OK && c.grad && c.dw) rc = sweep<T>(kSweepDw, a, rows, w, w_stride, parts, (T*)c.dw, c.dw_stride, stream);
+            if (rc == ND_OK && c.grad && c.dw)
+                rc = sweep<T>(kSweepDw, a, rows, w, w_stride, parts, (T*)c.dw, c.dw_stride, stream);
             return rc;
         }
     const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
@@ -1257,15 +1268,15 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
             else if (c.n > 0)
                 hipLaunchKernelGGL(probs_kernel<T>, all, dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)
-                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)(tiles * d_tiles * p.dw_shares)), dim3(kThreads), 0, stream, a, op, ox, v,
-                                   (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares, labels);
+                hipLaunchKernelGGL(dw_kernel<T>, dim3((unsigned)(tiles * d_tiles * p.dw_shares)), dim3(kThreads), 0, stream, a, op,
+                                   ox, v, (T*)c.dw, c.dw_stride, dw_parts, p.piece, p.dw_shares, labels);
             if (c.dw && p.dw_shares > 1)
-                hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here * join_columns), dim3(kThreads), 0, stream, a, dw_parts, p.dw_shares, p.piece, v,
-                                   here, (T*)c.dw, c.dw_stride, labels);
+                hipLaunchKernelGGL(dw_join_kernel<T>, wave_per(here * join_columns), dim3(kThreads), 0, stream, a, dw_parts,
+                                   p.dw_shares, p.piece, v, here, (T*)c.dw, c.dw_stride, labels);
             if (c.dx && c.n > 0) {
                 const int64_t share = (tiles * kTileM / kLeastShare + p.shares - 1) / p.shares * kLeastShare;
-                hipLaunchKernelGGL(dx_kernel<T>, dim3((unsigned)(p.n_pad / kTileM * d_tiles * p.shares)), dim3(kThreads), 0, stream, a, op, ow,
-                                   v, share, tiles * kTileM, (int)(v == 0), parts);
+                hipLaunchKernelGGL(dx_kernel<T>, dim3((unsigned)(p.n_pad / kTileM * d_tiles * p.shares)), dim3(kThreads), 0, stream,
+                                   a, op, ow, v, share, tiles * kTileM, (int)(v == 0), parts);
             }
         }
         if (c.dx && c.n > 0)

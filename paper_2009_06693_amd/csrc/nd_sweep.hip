@@ -83,7 +83,9 @@ struct SweepArgs {
 };
 
 template <typename T, int D, int MODE>
-__global__ __attribute__((amdgpu_waves_per_eu(Shape<MODE, D>::kWaves, Shape<MODE, D>::kWaves))) __launch_bounds__((Shape<MODE, D>::kThreads)) void sweep_kernel(LossArgs a, SweepArgs s) {
+__global__ __attribute__((amdgpu_waves_per_eu(Shape<MODE, D>::kWaves, Shape<MODE, D>::kWaves)))
+__launch_bounds__((Shape<MODE, D>::kThreads))
+void sweep_kernel(LossArgs a, SweepArgs s) {
     using Sh = Shape<MODE, D>;
     using V8 = typename Eight<T>::V;
     constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing, UNIT = Sh::kUnit;
@@ -122,7 +124,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(Shape<MODE, D>::kWaves, Shape<MODE
         }
 
     // behind what an instruction's offset reaches from the front of LDS: the lane's own places, kept in registers
-    LdsChar *factor_lds = unit_lds + RING * Sh::kUnitBytes + half * 16, *sign_lds = unit_lds + RING * Sh::kUnitBytes + UNIT * 4 + half * 8;
+    LdsChar *factor_lds = unit_lds + RING * Sh::kUnitBytes + half * 16,
+            *sign_lds = unit_lds + RING * Sh::kUnitBytes + UNIT * 4 + half * 8;
     if (MODE == kSweepDw) asm volatile("" : "+v"(factor_lds), "+v"(sign_lds));
 
     const int64_t end = deal.first((int64_t)blockIdx.x + 1);
@@ -212,7 +215,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(Shape<MODE, D>::kWaves, Shape<MODE
             } p;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int32_t at = kTight ? (column_at[0][0] ^ ((j & 3) * 64 + e * 32)) + e * 8 * D * 2 : column_at[kTight ? 0 : e][kTight ? 0 : j & 3];
+                const int32_t at = kTight ? (column_at[0][0] ^ ((j & 3) * 64 + e * 32)) + e * 8 * D * 2
+                                          : column_at[kTight ? 0 : e][kTight ? 0 : j & 3];
                 p.q[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsOf<Short4>*>(
                     unit_lds + at + (slot * Sh::kUnitBytes + (b * 32 + t * 16) * D * 2 + (j >> 2) * 256)));
             }
@@ -477,7 +481,8 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepPart
 constexpr int kFinishRows = 8;
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
-                                                          int64_t w_stride, SweepParts parts, T* __restrict__ dx, int64_t dx_stride) {
+                                                          int64_t w_stride, SweepParts parts, T* __restrict__ dx,
+                                                           int64_t dx_stride) {
     constexpr int HELD = sweep_shape(MODE, D).held();
     constexpr int PER = D / 64;     // numbers of a lane
     constexpr int kAtOnce = 5;      // labels' rows under way
@@ -493,7 +498,8 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
             const Piece<T, PER> x = load_piece<T, PER>(rows + p * D + e0);
             float top = kLowest, sum = 0.f;
             for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
-                const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile], t = fmaxf(top, t2);
+                const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile];
+                const float t = fmaxf(top, t2);
                 sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
                 top = t;
             }
@@ -580,7 +586,8 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
     if (kLds > 64 * 1024)
         ND_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&sweep_kernel<T, D, MODE>),
                                          hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
-    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(sweep_shape(MODE, D).groups()), dim3(Shape<MODE, D>::kThreads), kLds, stream, a, s);
+    hipLaunchKernelGGL((sweep_kernel<T, D, MODE>), dim3(sweep_shape(MODE, D).groups()), dim3(Shape<MODE, D>::kThreads),
+                       kLds, stream, a, s);
     ND_HIP_CHECK(hipGetLastError());
     return ND_OK;
 }
@@ -624,9 +631,11 @@ int sweep_finish(int mode, const LossArgs& a, const T* rows, const T* w, int64_t
         constexpr int D = decltype(width)::value;
         const dim3 grid = groups_for(a.n, kFinishRows), block(kThreads);
         if (mode == kSweepLse)
-            hipLaunchKernelGGL((finish_kernel<T, D, kSweepLse>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx, dx_stride);
+            hipLaunchKernelGGL((finish_kernel<T, D, kSweepLse>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx,
+                               dx_stride);
         else
-            hipLaunchKernelGGL((finish_kernel<T, D, kSweepDx>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx, dx_stride);
+            hipLaunchKernelGGL((finish_kernel<T, D, kSweepDx>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx,
+                               dx_stride);
         ND_HIP_CHECK(hipGetLastError());
         return ND_OK;
     });

@@ -165,6 +165,18 @@ def test_infinities_and_nan_stay_in_their_rows(kind, value):
     want.check(loss[keep], lse[keep], dx[keep])
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_infinities_and_nan_of_long_rows_stay_there(kind, value):
+    for d in (300, 520):
+        x, w, labels, row_weight = _inputs(140, 400, d, 1, TYPES[kind], seed=d, empty=0.0)
+        x[5, 3] = value
+        loss, lse, dx, _ = _run(*(t.to(DEV) for t in (x, w, labels, row_weight)))
+        assert not bool(loss[5].isfinite())
+        keep = torch.arange(140) != 5
+        Loss(x[keep], w, labels[keep], row_weight[keep]).check(loss[keep], lse[keep], dx[keep])
+
+
 def test_weights_of_rows():
     """None counts as one; zeros give zero gradients; very different ones keep the small rows' gradients."""
     for kind, dtype in TYPES.items():
