@@ -13,6 +13,8 @@ struct GroupSum {
     const int64_t* counts;    // live pairs and groups: the caller's two numbers,
     const StepCtl* ctl;       // what the grouping left, or (both null) all
     const int32_t* group_row; // row of the output by group (null: the group's number)
+    const int32_t* mark_key;  // both or none: mark[mark_key[group]] = group
+    int32_t* mark;
     int64_t n_pairs, n_groups, out_rows, out_stride;
     int32_t* tile_group;      // scratch: a group per tile of pairs
     float* parts;             // scratch: [tile][first, last][d]

@@ -301,6 +301,7 @@ __device__ __forceinline__ void mark_tiles(const GroupSum& g, int64_t groups, in
             last = (b - 1) / g.tile;
         }
     }
+    if (g.mark && u < groups) g.mark[g.mark_key[u]] = (int32_t)u;
     // few: every lane its own; many (a hub): the wavefront together
     uint64_t many = __ballot(last - first >= 8);
     if (last - first < 8)

@@ -166,6 +166,9 @@ __device__ __forceinline__ void pad_row(const T* __restrict__ from, T* __restric
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, Spread s, const T* __restrict__ x, int64_t x_stride,
                                                           T* __restrict__ rows, T* __restrict__ dx, int64_t dx_stride) {
+    if (a.label_row)  // none yet
+        for (int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x; v < a.V; v += (int64_t)gridDim.x * kThreads)
+            a.label_row[v] = -1;
     const uint32_t in_group = fastdiv(threadIdx.x, s.lanes), lane = threadIdx.x - in_group * s.lanes.d;
     if (in_group >= s.places) return;
     const int64_t live = a.header->n_live, padded = (live + kTile - 1) / kTile * kTile;
@@ -201,17 +204,6 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(const T* __restrict__ w, 
     if (in_group >= s.places) return;
     for (int64_t r = (int64_t)blockIdx.x * s.places + in_group; r < rows; r += (int64_t)gridDim.x * s.places)
         pad_row(w + r * stride, out + r * dp, d, dp, lane, s.lanes.d);
-}
-
-// Which row of the sums over labels is a vertex's: none, then those of the groups.
-__global__ __launch_bounds__(kThreads) void label_clear_kernel(int32_t* __restrict__ label_row, int64_t V) {
-    const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (v < V) label_row[v] = -1;
-}
-__global__ __launch_bounds__(kThreads) void label_rows_kernel(const StepCtl* __restrict__ ctl, const int32_t* __restrict__ key,
-                                                              int64_t most, int32_t* __restrict__ label_row) {
-    const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (u < most && u < (int64_t)ctl->U) label_row[key[u]] = (int32_t)u;
 }
 
 // ------------------------------------------------------------------------------------------------ product of tiles
@@ -1128,27 +1120,23 @@ int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, Sw
     const int64_t slots = a.n * a.k;
     StepCtl* ctl = (StepCtl*)(ws + p.o_ctl);
     int32_t *keys = nullptr, *vals = nullptr, *g_key = (int32_t*)(ws + p.o_gkey), *g_start = (int32_t*)(ws + p.o_gstart);
-    int32_t* label_row = (int32_t*)(ws + p.o_label_row);
     int rc = sort_pairs(a.labels_of, slots, (int32_t)a.V, p.sort, (int32_t*)(ws + p.o_keys[0]), (int32_t*)(ws + p.o_vals[0]),
                         (int32_t*)(ws + p.o_keys[1]), (int32_t*)(ws + p.o_vals[1]), (uint32_t*)(ws + p.o_hist), ctl, nullptr,
                         1, nullptr, &keys, &vals, stream);
     if (rc == ND_OK) rc = build_groups(keys, slots, ctl, g_key, g_start, (uint32_t*)(ws + p.o_scratch), nullptr, 0, stream);
     if (rc != ND_OK) return rc;
-    hipLaunchKernelGGL(label_clear_kernel, dim3((unsigned)((a.V + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream,
-                       label_row, a.V);
-    hipLaunchKernelGGL(label_rows_kernel, dim3((unsigned)((p.label_groups + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                       stream, ctl, g_key, p.label_groups, label_row);
-    ND_HIP_CHECK(hipGetLastError());
     GroupSum g{};
     g.slots = vals;
     g.start = g_start;
     g.ctl = ctl;
+    g.mark_key = g_key;
+    g.mark = a.label_row;
     g.n_pairs = slots;
     g.n_groups = g.out_rows = p.label_groups;
     g.out_stride = a.dp;
     g.tile_group = (int32_t*)(ws + p.o_tile_group);
     g.parts = (float*)(ws + p.o_label_parts);
-    parts->label_row = label_row;
+    parts->label_row = a.label_row;
     parts->label_sums = (const float*)(ws + p.o_label_sums);
     return group_sum_floats<T>(rows, a.dp, p.n_pad, a.dp, a.k, a.weight, g, (float*)(ws + p.o_label_sums), stream);
 }
@@ -1209,6 +1197,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         constexpr int kWide = kChunk / (int)sizeof(T);
         return c.d >= kWide ? run_few<T, kWide>(a, c, stream) : run_few<T, 1>(a, c, stream);
     }
+    if (sizeof(T) == 2 && c.grad && c.dw && c.n > 0) a.label_row = (int32_t*)(ws + p.o_label_row);
     T* rows = (T*)(ws + p.o_rows);
     const unsigned blocks = (unsigned)p.blocks;
     const Spread spread = make_spread(p.dp, kChunk / (int)sizeof(T));

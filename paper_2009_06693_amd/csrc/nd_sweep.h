@@ -81,6 +81,7 @@ struct LossArgs {
     float *part_max, *part_sum;  // [groups of vertices][n_pad]
     int32_t groups;
     FastDiv div_k;
+    int32_t* label_row;       // dw of 16-bit rows: by vertex, the row of the sums over its labels, or -1 (else null)
 };
 
 // Memory of a sweep's segments.
