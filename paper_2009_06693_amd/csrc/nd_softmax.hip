@@ -535,15 +535,22 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __r
         const float lse = top + logf(sum);
         const int64_t row = a.row_of[p];
         float met = 0.f;
-        for (int32_t j = 0; j < a.k; ++j) {
-            const int32_t v = a.labels_of[p * a.k + j];
-            if (v < 0) continue;
-            float dot = 0.f;
-            for (int32_t e = lane_id(); e < a.d; e += kWave)
-                dot = fmaf((float)rows[p * a.dp + e], (float)w[(int64_t)v * w_stride + e], dot);
-            for (int s = 32; s > 0; s >>= 1) dot += __shfl_xor(dot, s);
-            met += dot;
+        constexpr int kAtOnce = 4;  // labels' rows under way
+        for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
+            int32_t v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) v[j] = j0 + j < a.k ? a.labels_of[p * a.k + j0 + j] : -1;
+            for (int32_t e = lane_id(); e < a.d; e += kWave) {
+                const float mine = (float)rows[p * a.dp + e];
+                float of[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) of[j] = v[j] >= 0 ? (float)w[(int64_t)v[j] * w_stride + e] : 0.f;
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (v[j] >= 0) met = fmaf(mine, of[j], met);
+            }
         }
+        for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
         if (lane_id() == 0) {
             a.place_lse[p] = lse;
             a.lse[row] = lse;
