@@ -4,9 +4,10 @@
 //     dx_n = g_n (c_n sum_v p_nv w_v - sum_j w_label[n][j])     dw_v = sum_n g_n (c_n p_nv - #{j: label = v}) x_n
 //
 // Rows with labels are gathered once into a dense, zero-padded array, so that every product below works on full tiles of
-// rows that count, whatever rows without labels hold.  The logits are a matrix product whose tiles leave only a running
-// maximum and sum per row; for the gradient the tiles are made again, turned into g (c p - count), rounded to the rows'
-// type and multiplied by w (for dx) and by x (for dw), a piece of vertices at a time.
+// rows that count, whatever rows without labels hold.  The logits are a matrix product whose tiles leave a running maximum
+// and sum per row and, where rows are long, themselves; for the gradient what is kept, or made again a piece of vertices at a
+// time, is turned into a vertex's weight, rounded to the rows' type and multiplied by w (for dx) and by x (for dw).  Rows of
+// 16 bits that are short go through sweeps instead, and a few rows without gradient through a kernel of their own.
 #include <cfloat>
 #include <type_traits>
 
