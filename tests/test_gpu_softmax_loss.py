@@ -268,6 +268,29 @@ def test_replays_of_a_graph_and_two_streams(kind, d):
     assert all(torch.equal(x, y) for x, y in zip(b.grad(*other), want_b))
 
 
+@pytest.mark.parametrize("kind,n,d,grad", [("f16", 300, 520, True), ("f32", 300, 128, True), ("bf16", 3, 100, False),
+                                           ("f32", 40, 60, False)])
+def test_replays_over_long_and_few_rows(kind, n, d, grad):
+    V = 3000
+    args = [t.to(DEV) for t in _inputs(n, V, d, 2, TYPES[kind], seed=41)]
+    op = B.SoftmaxLoss(n, V, d, 2, TYPES[kind], grad=grad)
+    call = (lambda: op.grad(*args)) if grad else (lambda: op.loss(*args[:3]))
+    want = [t.clone() for t in call()]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        op.workspace.fill_(0xFF)
+        for t in got:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        assert all(torch.equal(x, y) for x, y in zip(call(), want))
+
+
 def test_gradient_against_differences():
     """Directional derivatives of the weighted sum of losses, by differences of the formula in 64 bits."""
     x, w, labels, row_weight = _inputs(60, 200, 96, 3, torch.float32, seed=41)
