@@ -442,8 +442,9 @@ typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
  * Up to 256 16-bit numbers a row no score leaves the registers.  Of longer rows, and in fp32, scores and what is made of
  * them lie in the workspace: at most 512 MB of probabilities at a time, or up to 4 GB of scores where rows are so long that
  * they are cheaper to keep than to make twice.  Before they are multiplied by rows, probabilities are rounded to the type of
- * the rows; what labels weigh is not (fp32: both stay in fp32).  fp16: row_weight p is held in steps no finer than 2^-39 k of
- * the largest finite row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status waits for the
+ * the rows (fp32: not at all), half a step relative to each.  A row's own labels are not: c_n p - #, small where a row is
+ * fitted, is made and multiplied in 32 bits.  fp16: row_weight p is held in steps no finer than 2^-39 k of the largest finite
+ * row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status waits for the
  * stream and returns ND_ERR_BAD_ROOT then.  Infinities and NaN in a row of x stay in that row's loss, lse and dx.
  * Limits: n < 2^30, V < 2^31, d <= ND_MAX_ROW, k <= ND_MAX_LABELS, n * k < 2^31.  Errors: ND_ERR_NULL_POINTER,
  * ND_ERR_BAD_ARGUMENT, ND_ERR_TOO_LARGE, ND_ERR_WORKSPACE, ND_ERR_HIP.

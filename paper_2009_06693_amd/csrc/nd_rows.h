@@ -21,7 +21,7 @@ struct GroupSum {
     int32_t tile;             // pairs of a tile (filled in)
 };
 
-// Sums in 32-bit floats, out[u] over group u of weights[q / m] x[q / m] (weights by row).
+// Sums in 32-bit floats, out[u] over group u of weights[q] x[q / m].
 template <typename T>
 int group_sum_floats(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
                      float* out, hipStream_t stream);

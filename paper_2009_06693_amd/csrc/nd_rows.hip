@@ -357,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void group_tiles_kernel(int32_t d, Deal t
         clear_rows<T, VEC>(g, groups, pairs, d, t, (blockIdx.x - tile_blocks) * kThreads, out);
 }
 
-template <typename T, typename O, int VEC, bool BY_ROW>
+template <typename T, typename O, int VEC>
 __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict__ x, int64_t x_stride, int32_t d, Deal t,
                                                              FastDiv m, uint32_t n_slots,
                                                              const float* __restrict__ weights, GroupSum g,
@@ -388,9 +388,8 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
                 v[i] = Piece<T, VEC>{};
                 f[i] = 0.f;
                 if (q[i] < n_slots) {
-                    const uint32_t r = fastdiv(q[i], m);
-                    v[i] = load_piece<T, VEC>(x + (int64_t)r * x_stride + at);
-                    f[i] = weights ? weights[BY_ROW ? r : q[i]] : 1.f;
+                    v[i] = load_piece<T, VEC>(x + (int64_t)fastdiv(q[i], m) * x_stride + at);
+                    f[i] = weights ? weights[q[i]] : 1.f;
                 }
             }
 #pragma unroll
@@ -521,7 +520,7 @@ GroupSumPlan plan_group_sum(int64_t n_pairs, int32_t d) {
 }
 
 
-template <typename T, typename O, int VEC, bool BY_ROW>
+template <typename T, typename O, int VEC>
 int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, GroupSum g, O* out,
                      hipStream_t stream) {
     const Deal t = make_deal(d, VEC);
@@ -534,7 +533,7 @@ int launch_group_sum(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t
         hipLaunchKernelGGL((group_tiles_kernel<O, VEC>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(kThreads), 0, stream,
                            d, t, g, tile_blocks, out);
     if (sums)
-        hipLaunchKernelGGL((group_sum_kernel<T, O, VEC, BY_ROW>), dim3(workgroups((tiles + t.rows - 1) / t.rows), deal_columns(t)),
+        hipLaunchKernelGGL((group_sum_kernel<T, O, VEC>), dim3(workgroups((tiles + t.rows - 1) / t.rows), deal_columns(t)),
                            dim3(deal_threads(t)), 0, stream, x, x_stride, d, t, make_fastdiv((uint32_t)m), (uint32_t)(n * m),
                            weights, g, out);
     if (g.n_groups > 0)
@@ -582,7 +581,7 @@ int64_t group_sum_tiles(int64_t n_pairs, int32_t d, int dtype) {
 template <typename T>
 int group_sum_floats(const T* x, int64_t x_stride, int64_t n, int32_t d, int32_t m, const float* weights, const GroupSum& g,
                      float* out, hipStream_t stream) {
-    return launch_group_sum<T, float, 16 / (int)sizeof(T), true>(x, x_stride, n, d, m, weights, g, out, stream);
+    return launch_group_sum<T, float, 16 / (int)sizeof(T)>(x, x_stride, n, d, m, weights, g, out, stream);
 }
 template int group_sum_floats<bf16_t>(const bf16_t*, int64_t, int64_t, int32_t, int32_t, const float*, const GroupSum&, float*,
                                       hipStream_t);
@@ -777,7 +776,7 @@ int nd_rows_group_sum(const void* x_dev, int64_t x_stride, int dtype, int64_t n,
         using T = std::remove_pointer_t<decltype(type)>;
         return by_width<T>(d, [&](auto width) -> int {
             constexpr int VEC = decltype(width)::value;
-            return launch_group_sum<T, T, VEC, false>((const T*)x_dev, x_stride, n, d, m, weights_dev, g, (T*)out_dev, stream);
+            return launch_group_sum<T, T, VEC>((const T*)x_dev, x_stride, n, d, m, weights_dev, g, (T*)out_dev, stream);
         });
     });
 }

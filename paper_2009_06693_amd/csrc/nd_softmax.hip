@@ -14,7 +14,6 @@
 #include "nd_philox.h"
 #include "nd_rows.h"
 #include "nd_sweep.h"
-#include "nd_wave.h"
 
 namespace nd {
 namespace {
@@ -179,13 +178,27 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(LossArgs a, Spread s, 
             pad_row(x + row * x_stride, rows + p * a.dp, a.d, a.dp, lane, s.lanes.d);
             for (int32_t j = (int32_t)lane; j < a.k; j += (int32_t)s.lanes.d) {
                 const int32_t v = a.labels[row * a.k + j];
-                a.labels_of[p * a.k + j] = v >= 0 && (int64_t)v < a.V ? v : -1;
+                const uint32_t mine = v >= 0 && (int64_t)v < a.V ? (uint32_t)v : ~0u;
+                int32_t to = j;
+                if (a.label_score) {  // ascending
+                    to = 0;
+#pragma unroll 4
+                    for (int32_t i = 0; i < a.k; ++i) {
+                        const int32_t u = a.labels[row * a.k + i];
+                        const uint32_t other = u >= 0 && (int64_t)u < a.V ? (uint32_t)u : ~0u;
+                        to += other < mine || (other == mine && i < j);
+                    }
+                }
+                a.labels_of[p * a.k + to] = (int32_t)mine;
             }
             continue;
         }
         if (p < padded) {
             pad_row((const T*)nullptr, rows + p * a.dp, 0, a.dp, lane, s.lanes.d);
-            if (lane == 0) a.count[p] = a.weight[p] = a.place_lse[p] = 0.f;
+            if (lane == 0) {
+                a.count[p] = a.weight[p] = a.place_lse[p] = 0.f;
+                if (a.place_factor) a.place_factor[p] = INFINITY;
+            }
         }
         for (int32_t j = (int32_t)lane; j < a.k; j += (int32_t)s.lanes.d) a.labels_of[p * a.k + j] = -1;
         if (p < a.n) {
@@ -427,9 +440,6 @@ __device__ __forceinline__ void store_tile(const AccTile& acc, float factor, O* 
         }
 }
 
-constexpr float kLog2e = 1.44269504088896340736f;
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-
 // Workgroups go round the eight XCDs, each with an L2 of its own: tiles next to each other, which share an operand, are
 // given to workgroups of one XCD.
 __device__ __forceinline__ int64_t tile_id() {
@@ -515,7 +525,47 @@ void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x,
         }
 }
 
-// lse and loss of the gathered rows, a wavefront each: parts joined, then the products with the labels' rows.
+// Scores of the labels of 16-bit rows, 32 a wavefront: the diagonal of a tile of places against their labels.  It takes a
+// thirty-second of what is computed, but has the numbers that the other products have, to the last bit: the same instructions
+// over the same operands (x's rows as the instruction's rows, or w's), in the same order.  Bound by fetching both rows.
+template <typename T, bool W_ROWS>
+__global__ __launch_bounds__(kThreads) void label_scores_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
+                                                                int64_t w_stride) {
+    constexpr int kAtOnce = 4;
+    const int lane = lane_id(), col = lane & 31, half = lane >> 5;
+    const int64_t slots = (int64_t)a.header->n_live * a.k;
+    for (int64_t s0 = ((int64_t)blockIdx.x * 4 + wave_id()) * 32; s0 < slots; s0 += (int64_t)gridDim.x * 128) {
+        const int64_t slot = s0 + col < slots ? s0 + col : slots - 1;
+        const int32_t label = a.labels_of[slot];
+        const T* of_x = rows + (int64_t)fastdiv((uint32_t)slot, a.div_k) * a.dp + half * 8;
+        const T* of_w = w + (int64_t)(label >= 0 ? label : 0) * w_stride + half * 8;
+        Acc acc = Acc{};
+        for (int32_t e = 0; e < a.dp; e += 16 * kAtOnce) {  // rows are padded to 64 numbers
+            Fragment<T> x[kAtOnce], v[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                x[i] = *reinterpret_cast<const Fragment<T>*>(of_x + e + i * 16);
+                v[i] = *reinterpret_cast<const Fragment<T>*>(of_w + e + i * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) acc = W_ROWS ? multiply(v[i], x[i], acc) : multiply(x[i], v[i], acc);
+        }
+        // row `col` of column `col`
+        float score = acc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) score = 8 * (r / 4) + r % 4 == (col & 27) ? acc[r] : score;
+        if (half == ((col >> 2) & 1) && s0 + col < slots) a.label_score[slot] = score;
+    }
+}
+
+// What a vertex weighs in a row's gradient: c p times the row's weight, scaled and rounded to the type.
+template <typename T>
+__device__ __forceinline__ T weight_of(float score, float lse, float count, float weight) {
+    return (T)(weight * (count * exp_of(score - lse)));
+}
+
+// lse and loss of the gathered rows, a wavefront each: parts joined, then the products with the labels' rows, or (scores of
+// labels are there) what labels weigh in the gradients.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                         int64_t w_stride) {
@@ -533,8 +583,27 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a, const T* __r
             sum = sum * exp_of(top - t) + s2 * exp_of(t2 - t);
             top = t;
         }
-        const float lse = top + logf(sum);
         const int64_t row = a.row_of[p];
+        if constexpr (!Kind<T>::kWide)
+            if (a.label_score) {
+                const int64_t slot = p * a.k + lane_id();
+                const bool mine = lane_id() < a.k;
+                const int32_t label = mine ? a.labels_of[slot] : -1;
+                const float score = label >= 0 ? a.label_score[slot] : 0.f, c = a.count[p], g = a.weight[p], scale = a.header->scale;
+                const LabelTerms terms = label_terms<false>(label, score, c, top, sum);
+                // The products round a label's weight with all others; it is made here to the last bit, so that taking it off
+                // again leaves what the label is in 32 bits.
+                const float rounded = (float)weight_of<T>(score, terms.lse, c, g * scale) * (1.f / scale);
+                if (mine) a.label_weight[slot] = terms.first ? g * terms.rate + rounded : 0.f;
+                float met = score;
+                for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
+                if (lane_id() == 0) {
+                    a.place_lse[p] = a.lse[row] = terms.lse;
+                    a.loss[row] = c * terms.lse - met;
+                }
+                continue;
+            }
+        const float lse = top + logf(sum);
         float met = 0.f;
         constexpr int kAtOnce = 4;  // labels' rows under way
         for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
@@ -718,7 +787,8 @@ __device__ __forceinline__ void count_labels(const LossArgs& a, int64_t v0, int6
 // What a vertex weighs in a row's gradient, as [vertex][row]: 256 vertices of the piece from v_first on, 128 rows.  In fp32
 // it is g (c p - count).  In 16 bits, to which it is rounded for the matrix instructions, it is g c p alone: one label can
 // outweigh all vertices, and the rounding of its count would be that of the whole gradient (fp16, relative to 64 bits, 3.2e-4
-// and without it 2.1e-4, which is the rounding of the result).  There the labels' rows are taken off afterwards, in 32 bits.
+// and without it 2.1e-4, which is the rounding of the result).  There the labels' rows are taken off afterwards, in 32 bits,
+// with the rounded g c p of theirs: where a row is fitted its rounding, 2^-9 of it in bf16, would outweigh g (c p - count).
 template <typename T>
 __global__ __attribute__((amdgpu_waves_per_eu(2, 2))) __launch_bounds__(kThreads)
 void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
@@ -748,9 +818,15 @@ void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
         for (int r = 0; r < 16; ++r) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float held = Kind<T>::kWide ? (float)counts[acc_col(j) * kCountPitch + acc_row(i, r)] : 0.f;
-                const bool counts_here = i * 32 + 8 * (r / 4) + r % 4 < left && c[j] > 0.f;
-                to[j * 32] = (T)(counts_here ? g[j] * (c[j] * exp_of(acc[i][j][r] - lse[j]) - held) : 0.f);
+                T weight = (T)0.f;
+                if (i * 32 + 8 * (r / 4) + r % 4 < left && c[j] > 0.f) {
+                    if constexpr (Kind<T>::kWide)
+                        weight = g[j] * (c[j] * exp_of(acc[i][j][r] - lse[j]) -
+                                         (float)counts[acc_col(j) * kCountPitch + acc_row(i, r)]);
+                    else
+                        weight = weight_of<T>(acc[i][j][r], lse[j], c[j], g[j]);
+                }
+                to[j * 32] = weight;
             }
             to += (r % 4 == 3 ? 5 : 1) * a.n_pad;
             asm volatile("" : "+v"(to));
@@ -785,8 +861,13 @@ __global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float*
             Piece<T, 4> p;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float held = Kind<T>::kWide ? (float)counts[(col + e) * kCountPitch + row] : 0.f;
-                p.v[e] = (T)(v0 + row < a.V && c[e] > 0.f ? g[e] * (c[e] * exp_of(s[i].v[e] - lse[e]) - held) : 0.f);
+                p.v[e] = (T)0.f;
+                if (v0 + row < a.V && c[e] > 0.f) {
+                    if constexpr (Kind<T>::kWide)
+                        p.v[e] = g[e] * (c[e] * exp_of(s[i].v[e] - lse[e]) - (float)counts[(col + e) * kCountPitch + row]);
+                    else
+                        p.v[e] = weight_of<T>(s[i].v[e], lse[e], c[e], g[e]);
+                }
             }
             store_piece<T, 4>(probs + (v0 + row) * a.n_pad + n0 + col, p);
         }
@@ -942,19 +1023,22 @@ __global__ __launch_bounds__(kThreads) void dx_join_kernel(LossArgs a, const flo
             constexpr int kAtOnce = 4;
             for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
                 Piece<T, 4> v[kAtOnce];
+                float f[kAtOnce];
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     const int32_t label = j0 + j < a.k ? a.labels_of[p * a.k + j0 + j] : -1;
                     v[j] = Piece<T, 4>{};
-                    if (label >= 0) v[j] = load_piece<T, 4>(w.base + label * w.stride + e);
+                    f[j] = 0.f;
+                    if (label >= 0) {
+                        v[j] = load_piece<T, 4>(w.base + label * w.stride + e);
+                        f[j] = a.label_weight[p * a.k + j0 + j];
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) less[q] += (float)v[j].v[q];
+                    for (int q = 0; q < 4; ++q) less[q] = fmaf(f[j], (float)v[j].v[q], less[q]);
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) less[q] *= a.weight[p];
         }
         join_parts<T>(parts + p * a.dp, shares, a.n_pad * a.dp, back, less, e, a.d, dx + a.row_of[p] * dx_stride);
     }
@@ -979,6 +1063,7 @@ struct LossPlan {
     SortPlan sort;
     size_t o_ctl, o_keys[2], o_vals[2], o_hist, o_scratch, o_gkey, o_gstart, o_label_row, o_label_sums, o_tile_group,
         o_label_parts;
+    size_t o_label_score, o_label_weight, o_factor;
     size_t o_labels, o_live, o_weight, o_bad, o_row, o_count, o_gweight, o_lse, o_max, o_sum, o_rows, o_w, o_probs, o_scores,
         o_parts, o_dw_parts, total;
 };
@@ -1049,6 +1134,9 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     p.o_w = take((size_t)V * (size_t)p.dp * (size_t)b);
     auto take_labels = [&] {
         const size_t slots = (size_t)n * (size_t)k, some = slots > 0 ? slots : 1;
+        p.o_label_score = take(some * 4);
+        p.o_label_weight = take(some * 4);
+        p.o_factor = take((size_t)p.n_pad * 4);
         const size_t tiles = (size_t)group_sum_tiles((int64_t)slots, p.dp, dtype);
         p.label_groups = (int64_t)slots < V ? (int64_t)slots : V;
         p.sort = make_sort_plan((int64_t)slots, V);
@@ -1122,7 +1210,7 @@ struct LossCall {
     bool grad;
 };
 
-// The rows under every vertex that is a label, summed: the part of dw that labels have.
+// The rows under every vertex that is a label, times what they weigh, summed: what labels take off dw.
 template <typename T>
 int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, SweepParts* parts, hipStream_t stream) {
     const int64_t slots = a.n * a.k;
@@ -1146,7 +1234,7 @@ int sum_labels(const LossArgs& a, const LossPlan& p, char* ws, const T* rows, Sw
     g.parts = (float*)(ws + p.o_label_parts);
     parts->label_row = a.label_row;
     parts->label_sums = (const float*)(ws + p.o_label_sums);
-    return group_sum_floats<T>(rows, a.dp, p.n_pad, a.dp, a.k, a.weight, g, (float*)(ws + p.o_label_sums), stream);
+    return group_sum_floats<T>(rows, a.dp, p.n_pad, a.dp, a.k, a.label_weight, g, (float*)(ws + p.o_label_sums), stream);
 }
 
 template <typename T, int VEC, int N>
@@ -1205,7 +1293,12 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         constexpr int kWide = kChunk / (int)sizeof(T);
         return c.d >= kWide ? run_few<T, kWide>(a, c, stream) : run_few<T, 1>(a, c, stream);
     }
-    if (sizeof(T) == 2 && c.grad && c.dw && c.n > 0) a.label_row = (int32_t*)(ws + p.o_label_row);
+    if (sizeof(T) == 2 && c.grad && c.n > 0) {
+        if (c.dw) a.label_row = (int32_t*)(ws + p.o_label_row);
+        a.label_score = (float*)(ws + p.o_label_score);
+        a.label_weight = (float*)(ws + p.o_label_weight);
+        if (p.sweep) a.place_factor = (float*)(ws + p.o_factor);
+    }
     T* rows = (T*)(ws + p.o_rows);
     const unsigned blocks = (unsigned)p.blocks;
     const Spread spread = make_spread(p.dp, kChunk / (int)sizeof(T));
@@ -1225,10 +1318,18 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
         w = padded;
         w_stride = p.dp;
     }
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
+        if (a.label_score) {
+            const int64_t groups = (c.n * c.k + 127) / 128;
+            const dim3 grid((unsigned)(groups < (1 << 20) ? groups : 1 << 20));
+            if (p.sweep)
+                hipLaunchKernelGGL((label_scores_kernel<T, false>), grid, dim3(kThreads), 0, stream, a, rows, w, w_stride);
+            else
+                hipLaunchKernelGGL((label_scores_kernel<T, true>), grid, dim3(kThreads), 0, stream, a, rows, w, w_stride);
+        }
         if (p.sweep) {
             SweepParts parts{a.part_max, a.part_sum, (float*)(ws + p.o_parts), nullptr, nullptr};
-            const int mode = c.grad && c.dx ? kSweepDx : kSweepLse;
+            const int mode = !c.grad ? kSweepLse : c.dx ? kSweepDx : kSweepRest;
             int rc = ND_OK;
             if (c.n > 0) {
                 rc = sweep<T>(mode, a, rows, w, w_stride, parts, nullptr, 0, stream);
@@ -1239,6 +1340,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
                 rc = sweep<T>(kSweepDw, a, rows, w, w_stride, parts, (T*)c.dw, c.dw_stride, stream);
             return rc;
         }
+    }
     const Operand<T> ow{w, w_stride, c.V, p.dp}, ox{rows, p.dp, p.n_pad, p.dp};
     if (c.n > 0) {
         hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(p.n_pad / kTile * p.groups)), dim3(kThreads), 0, stream, a, ow, ox,

@@ -2,26 +2,30 @@
 
 #include <type_traits>
 
-#include "nd_wave.h"
-
 // With h a tile of held rows and p a block of 32 passing rows, a wavefront makes
 //
-//     S[p][h] = p . h,    P = exp(S - top) or g (c exp(S - lse) - count),    O[h] += sum_p P[p][h] p
+//     S[p][h] = p . h,    P = exp(S - top), 0 where p is a label of h, or g c exp(S - lse),    O[h] += sum_p P[p][h] p
 //
 // in 32 x 32 x 16 matrix instructions.  S is made with the passing rows as the instruction's rows, so that a lane holds 16
 // passing rows of one held row: maxima and sums stay inside the lane, and the rounded P is at once the operand of
 // the second product, whose other operand, the passing rows read down their columns, comes from the same tile in LDS
 // through transposing reads.
 //
+// P is rounded to the rows' type for that product, relative to each P: with bf16 dx and dw move by 6.4e-4 and 6.0e-4 of their
+// size against weights in 32 bits (8,192 x 57,000 x 128), below their own rounding, and stay 1.66e-3 from 64 bits as they are
+// with those.  The remainder would be a third product, half as much work again.  It does not hold for a row's own labels, whose
+// P stands against a count: dx leaves them out and gets them back where the segments are joined; dw takes off, for every label,
+// what it rounded to and the difference from the count, both in 32 bits.
+//
 // What bounds it: matrix instructions and vector instructions share a SIMD's issue (an instruction of 32 cycles keeps it for
-// 16), and under both the clock falls below 2 GHz.  8,192 x 57,000 x 128 bf16: with dx 229 us, dw 238, 1,044 and 1,004 TFLOP/s
-// of products beside an exponential for every score; forward, 14,250 x 57,000 x 128 fp16, 229 us, 908; 8,192 x 233,000 x 256
-// 1,670 and 1,880 us.
+// 16), and under both the clock falls below 2 GHz.  8,192 x 57,000 x 128 bf16: with dx 260 us (225 where no label is left out; here
+// 74,000 are, two fifths of them in an eighth of the vertices, and the workgroups that sweep those end last), dw 231, 920 and
+// 1,035 TFLOP/s of products beside an exponential for every score; forward, 14,250 x 57,000 x 128 fp16, 229 us, 908; 8,192 x
+// 233,000 x 256 1,670 and 1,880 us.
 namespace nd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -1e38f;  // below every maximum, and finite times log2 e
 
 typedef float Acc __attribute__((ext_vector_type(16)));
@@ -49,7 +53,7 @@ struct Shape {
     static constexpr int kHeld = kShape.held();
     // A block's scores are made while the block before is still being worked on, where there are registers for both
     // (of 256: D / 8 for the held rows, D / 2 for the sums, 16 + 8 per block under way) and no second workgroup to fill in.
-    static constexpr bool kAhead = MODE != kSweepLse && D <= 128 && kShape.per_cu == 1;
+    static constexpr bool kAhead = MODE > kSweepRest && D <= 128 && kShape.per_cu == 1;
     static constexpr int kRing = kAhead ? 4 : 2;       // units in LDS
     static constexpr int kSteps = D / 16;              // instructions along a row
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
@@ -94,7 +98,8 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
     using Sh = Shape<MODE, D>;
     using V8 = typename Eight<T>::V;
     constexpr int HELD = Sh::kHeld, STEPS = Sh::kSteps, THREADS = Sh::kThreads, RING = Sh::kRing, UNIT = Sh::kUnit;
-    constexpr bool kSums = MODE != kSweepLse, kOnline = MODE != kSweepDw, kAhead = Sh::kAhead;
+    constexpr bool kSums = MODE > kSweepRest, kOnline = MODE != kSweepDw, kAhead = Sh::kAhead;
+    constexpr bool kApart = MODE == kSweepRest || MODE == kSweepDx;  // a row's labels are left out
     // fp16 ends at 2^-24: exponentials are taken times 2^8 and may outgrow the maximum that they are relative to by 2^6
     constexpr float kRaise = std::is_same<T, f16_t>::value ? 8.f : 0.f;
     constexpr float kMost = std::is_same<T, f16_t>::value ? 16384.f : 64.f;  // 2^6 times that
@@ -143,7 +148,7 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
 
         // ---- passing rows on their way to LDS
         Word4 ahead[Sh::kLoads];
-        float factor_ahead[3];
+        float factor_ahead[2];
         auto load = [&](int32_t u) {
             // No branches: what is loaded must not be waited for here.  Rows behind the last one are the last one again;
             // gathered rows are padded with zeros to whole units, but no further.
@@ -159,9 +164,8 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
             }
             if (MODE == kSweepDw) {
                 const int64_t p = from_row + (threadIdx.x & (UNIT - 1));
-                factor_ahead[0] = a.place_lse[p];
-                factor_ahead[1] = a.count[p];
-                factor_ahead[2] = a.weight[p];
+                factor_ahead[0] = a.place_factor[p];
+                factor_ahead[1] = a.weight[p];
             }
         };
         auto keep = [&](int32_t u, int slot) {
@@ -172,11 +176,10 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
             }
             if (MODE == kSweepDw && threadIdx.x < UNIT) {
                 // behind the segment's last unit nothing weighs
-                // g c exp(s - lse) = sign(g c) exp2(s log2 e - (lse log2 e - log2 |g c|))
-                const float gc = factor_ahead[1] * factor_ahead[2] * scale;
+                // g c exp(s - lse) = sign(g) exp2(s log2 e - (lse log2 e - log2 |g c|))
                 char* f = factors + slot * Sh::kFactorBytes;
-                reinterpret_cast<float*>(f)[threadIdx.x] = u < u1 ? factor_ahead[0] * kLog2e - log2f(fabsf(gc)) : INFINITY;
-                reinterpret_cast<uint16_t*>(f + UNIT * 4)[threadIdx.x] = gc < 0.f ? 0x8000 : 0;
+                reinterpret_cast<float*>(f)[threadIdx.x] = u < u1 ? factor_ahead[0] : INFINITY;
+                reinterpret_cast<uint16_t*>(f + UNIT * 4)[threadIdx.x] = factor_ahead[1] < 0.f ? 0x8000 : 0;
             }
         };
 
@@ -188,6 +191,19 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
 #pragma unroll
             for (int k = 0; k < STEPS; ++k)
                 rows[k] = *reinterpret_cast<const V8*>(held + r * s.held_stride + k * 16 + half * 8);
+        }
+        // ---- the first label of the lane's held row from the segment's first passing row on, the one after it, and how many
+        // of the row's are left from the next one on
+        uint32_t label = ~0u, label_after = ~0u;
+        int32_t labels_left = 0;
+        if (kApart && row0 + col < held_rows) {
+            const int32_t* labels = a.labels_of + (row0 + col) * a.k;
+            int32_t before = 0;
+#pragma unroll 4
+            for (int32_t j = 0; j < a.k; ++j) before += (uint32_t)labels[j] < (uint32_t)u0 * UNIT;
+            if (before < a.k) label = (uint32_t)labels[before];
+            if (before + 1 < a.k) label_after = (uint32_t)labels[before + 1];
+            labels_left = a.k - before - 1;
         }
         Acc sums[D / 32];
 #pragma unroll
@@ -273,6 +289,26 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
             for (int r = 0; r < 16; ++r)
                 if (half * 4 >= rows_left - (b * 32 + 8 * (r / 4) + r % 4)) now[r] = -INFINITY;
         };
+        // ---- Labels among the block's rows weigh nothing here: what they are in the gradient is put together in 32 bits where
+        // the segments are joined.  Few blocks hold one: the others cost a comparison.
+        auto leave_out = [&](Acc& now, int32_t u, int b) {
+            const uint32_t first = (uint32_t)u * UNIT + (uint32_t)b * 32u;
+            if (!__ballot(label - first < 32u)) return;
+            uint32_t found = 0;
+            do {
+                if (label - first < 32u) {
+                    found |= 1u << (label - first);
+                    label = label_after;
+                    label_after = ~0u;
+                    // the row's last labels_left, without the one that moved up
+                    if (--labels_left > 0) label_after = (uint32_t)a.labels_of[(row0 + col + 1) * a.k - labels_left];
+                }
+            } while (__ballot(label - first < 32u));
+            found >>= half * 4;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (found & (1u << (8 * (r / 4) + r % 4))) now[r] = -INFINITY;
+        };
         // ---- weights of a block from its scores, share i of them
         constexpr int kShare = kAhead ? 16 / STEPS : 4;
         float part;  // the block's sum
@@ -354,6 +390,7 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
                 if (kTight) __builtin_amdgcn_sched_barrier(0);  // what the steps read of LDS takes turns in the registers left
                 if (kOnline) {
                     mask(now, u, b);
+                    if (kApart) leave_out(now, u, b);
                     if (kAhead)
                         scores_and_sums(score[b ^ 1], next_slot, b ^ 1, weight[b ^ 1], before_slot, b ^ 1,
                                         [&](int i) { weights_of(now, mine, i); });
@@ -482,7 +519,7 @@ __global__ __launch_bounds__(kThreads) void dw_join_kernel(LossArgs a, SweepPart
     }
 }
 
-// lse, loss and dx of the gathered rows, a wavefront each at a time; a workgroup's are of one tile.
+// lse, loss and dx of the gathered rows and what labels weigh in dw, a wavefront each at a time; a workgroup's are of one tile.
 constexpr int kFinishRows = 8;
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
@@ -491,6 +528,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
     constexpr int HELD = sweep_shape(MODE, D).held();
     constexpr int PER = D / 64;     // numbers of a lane
     constexpr int kAtOnce = 5;      // labels' rows under way
+    constexpr bool kApart = MODE != kSweepLse;  // labels are not in the segments' sums
     const int64_t live = a.header->n_live;
     const SweepDeal deal(live, a.V, sweep_shape(MODE, D));
     const int e0 = lane_id() * PER;
@@ -500,7 +538,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
         for (int64_t p = p0 + wave_id(); p < p0 + kFinishRows && p < live; p += 4) {
             const int64_t in_tile = p % HELD, row = a.row_of[p];
             const int32_t my_label = lane_id() < a.k ? a.labels_of[p * a.k + lane_id()] : -1;
-            const Piece<T, PER> x = load_piece<T, PER>(rows + p * D + e0);
+            const float my_score = kApart && my_label >= 0 ? a.label_score[p * a.k + lane_id()] : 0.f;
             float top = kLowest, sum = 0.f;
             for (int64_t g = g0 + lane_id(); g <= g1; g += kWave) {
                 const float t2 = parts.top[(g + tile) * HELD + in_tile], s2 = parts.sum[(g + tile) * HELD + in_tile];
@@ -513,46 +551,79 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(LossArgs a, const T* _
                 sum = sum * exp2_of((top - t) * kLog2e) + s2 * exp2_of((t2 - t) * kLog2e);
                 top = t;
             }
-            const float lse = top + logf(sum), c = a.count[p];
-            float grad[PER] = {};
-            if (MODE == kSweepDx) {
+            const float c = a.count[p];
+            float lse, met;
+            LabelTerms terms;
+            if constexpr (kApart) {
+                terms = label_terms<true>(my_label, my_score, c, top, sum);
+                lse = terms.lse;
+                met = my_score;
+            } else {
+                lse = top + logf(sum);
+                met = 0.f;
+                const Piece<T, PER> x = load_piece<T, PER>(rows + p * D + e0);
+                for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
+                    Piece<T, PER> r[kAtOnce];
+                    int32_t v[kAtOnce];
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        v[j] = j0 + j < a.k ? __builtin_amdgcn_readlane(my_label, j0 + j) : -1;
+                        r[j] = Piece<T, PER>{};
+                        if (v[j] >= 0) r[j] = load_piece<T, PER>(w + (int64_t)v[j] * w_stride + e0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                        for (int i = 0; i < PER; ++i)
+                            if (v[j] >= 0) met = fmaf((float)x.v[i], (float)r[j].v[i], met);
+                }
+            }
+            for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
+            if (lane_id() == 0) {
+                a.lse[row] = lse;
+                a.loss[row] = c * lse - met;
+            }
+            if constexpr (kApart) {
+                // In dw the sweep rounds a label's weight with all others; it is made here to the last bit, so that taking it off
+                // again leaves what the label is in 32 bits.
+                const float g = a.weight[p], scale = a.header->scale, factor = lse * kLog2e - log2f(fabsf(c * g * scale));
+                const float rounded = (float)(T)exp2_of(fmaf(my_score, kLog2e, -factor)) * (1.f / scale);
+                if (lane_id() == 0) a.place_factor[p] = factor;
+                if (lane_id() < a.k)
+                    a.label_weight[p * a.k + lane_id()] = terms.first ? g * terms.rate + (g < 0.f ? -rounded : rounded) : 0.f;
+            }
+            if constexpr (MODE == kSweepDx) {
+                float grad[PER] = {};
 #pragma unroll 4
                 for (int64_t g = g0; g <= g1; ++g) {
                     const int64_t at = (g + tile) * HELD + in_tile;
-                    const float f = exp2_of((parts.top[at] - top) * kLog2e);
+                    const float f = exp2_of((parts.top[at] - terms.top) * kLog2e);
                     const Piece<float, PER> v = load_piece<float, PER>(parts.rows + at * D + e0);
 #pragma unroll
                     for (int i = 0; i < PER; ++i) grad[i] = fmaf(f, v.v[i], grad[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < PER; ++i) grad[i] *= c / sum;
-            }
-            float met = 0.f;
-            for (int32_t j0 = 0; j0 < a.k; j0 += kAtOnce) {
-                Piece<T, PER> r[kAtOnce];
-                int32_t v[kAtOnce];
+                for (int i = 0; i < PER; ++i) grad[i] *= c / terms.total;
+                uint64_t left = __ballot(terms.first);
+                while (left) {
+                    Piece<T, PER> r[kAtOnce];
+                    float rate[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    v[j] = j0 + j < a.k ? __builtin_amdgcn_readlane(my_label, j0 + j) : -1;
-                    r[j] = Piece<T, PER>{};
-                    if (v[j] >= 0) r[j] = load_piece<T, PER>(w + (int64_t)v[j] * w_stride + e0);
-                }
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        if (v[j] < 0) continue;
-                        met = fmaf((float)x.v[i], (float)r[j].v[i], met);
-                        grad[i] -= (float)r[j].v[i];
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        r[j] = Piece<T, PER>{};
+                        rate[j] = 0.f;
+                        if (left) {
+                            const int from = __ffsll((unsigned long long)left) - 1;
+                            left &= left - 1;
+                            rate[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(terms.rate), from));
+                            r[j] = load_piece<T, PER>(w + (int64_t)__builtin_amdgcn_readlane(my_label, from) * w_stride + e0);
+                        }
                     }
-            }
-            for (int s = 32; s > 0; s >>= 1) met += __shfl_xor(met, s);
-            if (lane_id() == 0) {
-                a.place_lse[p] = lse;
-                a.lse[row] = lse;
-                a.loss[row] = c * lse - met;
-            }
-            if (MODE == kSweepDx) {
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) grad[i] = fmaf(-rate[j], (float)r[j].v[i], grad[i]);
+                }
                 const float g = a.weight[p];
                 Piece<T, PER> o;
 #pragma unroll
@@ -619,6 +690,7 @@ int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stri
     return by_width(a.dp, [&](auto width) -> int {
         constexpr int D = decltype(width)::value;
         if (mode == kSweepLse) return launch_sweep<T, D, kSweepLse>(a, s, stream);
+        if (mode == kSweepRest) return launch_sweep<T, D, kSweepRest>(a, s, stream);
         if (mode == kSweepDx) return launch_sweep<T, D, kSweepDx>(a, s, stream);
         const int rc = launch_sweep<T, D, kSweepDw>(a, s, stream);
         if (rc != ND_OK) return rc;
@@ -637,6 +709,9 @@ int sweep_finish(int mode, const LossArgs& a, const T* rows, const T* w, int64_t
         const dim3 grid = groups_for(a.n, kFinishRows), block(kThreads);
         if (mode == kSweepLse)
             hipLaunchKernelGGL((finish_kernel<T, D, kSweepLse>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx,
+                               dx_stride);
+        else if (mode == kSweepRest)
+            hipLaunchKernelGGL((finish_kernel<T, D, kSweepRest>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx,
                                dx_stride);
         else
             hipLaunchKernelGGL((finish_kernel<T, D, kSweepDx>), grid, block, 0, stream, a, rows, w, w_stride, parts, dx,
