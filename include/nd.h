@@ -476,8 +476,9 @@ int nd_softmax_loss_status(const void* workspace_dev, void* hip_stream);
  *                       vertices sums their rows out of a table (a GraphSAGE aggregator; m = 1: a look-up)
  * nd_rows_weight_grad   dweights[r m + j] = dy_r . z_index[r m + j], 0 where nd_rows_to_samples skips
  * nd_rows_group_sum     out_u = sum over the pairs p of group u, those from group_start[u] to group_start[u + 1]
- *                       (n_groups + 1 offsets that do not descend, as nd_group_by_transit gives them), of weights[q]
- *                       x_(q div m), q = sorted_slots[p]: the gradient of rows that several slots read.  group_row_dev
+ *                       (n_groups + 1 offsets that do not descend, as nd_group_by_transit gives them, or a part of those
+ *                       with all pairs: pairs before the first offset are in no group), of weights[q] x_(q div m),
+ *                       q = sorted_slots[p]: the gradient of rows that several slots read.  group_row_dev
  *                       NULL: out has n_groups rows; otherwise (device, nd_group_by_transit's group_transit: ascending,
  *                       none twice) group u's sum is row group_row[u] of out, and the others of its out_rows rows are 0.
  *                       A group without pairs is a row of zeros.  Fewer than 2^31 groups and rows of out

@@ -514,8 +514,9 @@ def nd_rows_group_sum(x: torch.Tensor, sorted_slots: torch.Tensor, group_start: 
                       num_rows: Optional[int] = None, counts: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
-    """Sums per group of weights[q] * x[q // m]; group_start int32 [groups + 1].  With group_rows (int32 [groups],
-    ascending: the grouping's transits) the sums are those rows of a table of num_rows, whose other rows are 0."""
+    """Sums per group of weights[q] * x[q // m]; group_start int32 [groups + 1], a whole grouping's or a part of it.  With
+    group_rows (int32 [groups], ascending: the grouping's transits) the sums are those rows of a table of num_rows, whose other
+    rows are 0."""
     return _rows_call("group_sum", stream, x, sorted_slots, group_start, m, weights, group_rows, num_rows, counts, out,
                       workspace)
 

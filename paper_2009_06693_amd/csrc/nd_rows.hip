@@ -291,13 +291,14 @@ __device__ __forceinline__ int64_t row_of_group(const GroupSum& g, int64_t u) {
     return r >= 0 && r < g.out_rows ? r : -1;
 }
 
-// Which group every tile begins in.
+// Which group the first pair in a tile that is in one belongs to: the tile's first pair, or, where the offsets begin behind it,
+// the first group's.  Tiles in front of that are not marked, and not read.
 __device__ __forceinline__ void mark_tiles(const GroupSum& g, int64_t groups, int64_t pairs, int64_t u) {
-    int64_t first = 0, last = -1;  // tiles whose first pair is this group's
+    int64_t first = 0, last = -1;  // the group's tiles
     if (u < groups) {
         const int64_t a = start_of(g, u, pairs), b = start_of(g, u + 1, pairs);
         if (b > a) {
-            first = (a + g.tile - 1) / g.tile;
+            first = a > start_of(g, 0, pairs) ? (a + g.tile - 1) / g.tile : a / g.tile;
             last = (b - 1) / g.tile;
         }
     }
@@ -366,9 +367,12 @@ __global__ __launch_bounds__(kThreads) void group_sum_kernel(const T* __restrict
     int32_t at;
     if (!deal_lane<VEC>(t, d, &row, &at)) return;
     const uint32_t groups = (uint32_t)live_groups(g), pairs = (uint32_t)grouped_pairs(g, groups);
+    const uint32_t first_pair = groups > 0 ? (uint32_t)start_of(g, 0, pairs) : 0;  // those before it are in no group
     for (int64_t tile = (int64_t)blockIdx.x * t.rows + row; tile * g.tile < pairs; tile += (int64_t)gridDim.x * t.rows) {
-        const uint32_t p0 = (uint32_t)(tile * g.tile);
-        const uint32_t p1 = pairs - p0 < (uint32_t)g.tile ? pairs : p0 + g.tile;
+        const uint32_t tile_first = (uint32_t)(tile * g.tile);
+        const uint32_t p1 = pairs - tile_first < (uint32_t)g.tile ? pairs : tile_first + g.tile;
+        if (p1 <= first_pair) continue;
+        const uint32_t p0 = tile_first < first_pair ? first_pair : tile_first;
         uint32_t u = (uint32_t)g.tile_group[tile];
         if (u >= groups) u = groups - 1;
         bool before = start_of(g, u, pairs) < p0;
