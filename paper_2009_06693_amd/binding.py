@@ -425,7 +425,9 @@ def layer_edges(g: Graph, transits: torch.Tensor, sampled: torch.Tensor, stream=
 
 
 # ---------------------------------------------------------------------------
-# Rows of features: 2-D CUDA tensors of float32, bfloat16 or float16 whose rows lie in one piece, at any stride.
+# Rows of features: 2-D CUDA tensors of float32, bfloat16 or float16 whose rows lie in one piece, at any stride.  Autograd does
+# not see these calls: tensors that require a gradient are taken as their numbers, and results carry no graph.  Every call's
+# gradient is a call of its own.
 # ---------------------------------------------------------------------------
 
 def _place(stream: Optional[torch.cuda.Stream]):
@@ -462,7 +464,8 @@ def nd_softmax_loss_workspace_bytes(n: int, V: int, d: int, k: int, dtype: torch
 
 def nd_softmax_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
                     workspace: torch.Tensor, stream=None):
-    """x [n, d], w [V, d], labels int32 [n] or [n, k]; loss and lse float32 [n] are written."""
+    """x [n, d], w [V, d], labels int32 [n] or [n, k]; loss and lse float32 [n] are written (of longer ones the first n).
+    Gradients come from nd_softmax_loss_grad, not from autograd."""
     _rows_call("softmax_loss", stream, x, w, labels, loss, lse, workspace)
 
 
@@ -522,7 +525,11 @@ def nd_rows_group_sum(x: torch.Tensor, sorted_slots: torch.Tensor, group_start: 
 
 
 class SoftmaxLoss:
-    """Workspace and outputs of the softmax loss for calls of one shape."""
+    """Workspace and outputs of the softmax loss for calls of one shape.
+
+    loss() and grad() return this object's own tensors: the next call writes over what the last one returned, so clone what has
+    to stay.  Autograd does not see the calls; grad() returns the gradients.
+    """
 
     def __init__(self, n: int, V: int, d: int, k: int, dtype: torch.dtype, grad: bool = False, device="cuda:0"):
         self.workspace_bytes = nd_softmax_loss_workspace_bytes(n, V, d, k, dtype, grad)
@@ -533,12 +540,12 @@ class SoftmaxLoss:
         self._dw = torch.empty((V, d), dtype=dtype, device=device) if grad else None
 
     def loss(self, x, w, labels, stream=None):
-        """(loss, lse) per row."""
+        """(loss, lse) per row of x, which may have fewer rows than were planned for."""
         nd_softmax_loss(x, w, labels, self._loss, self._lse, self.workspace, stream)
-        return self._loss, self._lse
+        return self._loss[:x.shape[0]], self._lse[:x.shape[0]]
 
     def grad(self, x, w, labels, row_weight=None, stream=None):
-        """(loss, lse, dx, dw)."""
+        """(loss, lse, dx, dw); x has as many rows as were planned for, w too."""
         nd_softmax_loss_grad(x, w, labels, row_weight, self._loss, self._lse, self._dx, self._dw, self.workspace, stream)
         return self._loss, self._lse, self._dx, self._dw
 
