@@ -69,6 +69,60 @@ __global__ __launch_bounds__(kTile) void count_kernel(LossArgs a) {
     }
 }
 
+template <typename T>
+__device__ __forceinline__ void write_header(const LossArgs& a, uint32_t live, uint32_t bad, float top) {
+    a.header->status = bad;
+    a.header->n_live = live;
+    // fp16 holds 2^-24 to 65,504: the largest product of a weight and a count of labels becomes at most 2^15
+    float scale = 1.f;
+    if (std::is_same<T, f16_t>::value && top > 0.f)
+        scale = exp2f(fminf(fmaxf(floorf(log2f(32768.f / (float)a.k) - log2f(top)), -60.f), 60.f));
+    a.header->scale = scale;
+}
+
+// Many blocks: each block's count becomes that of the blocks before it, by one workgroup, which also writes the header.  Up to
+// kScanBlocks every block adds up what is before it by itself, a launch less and as many reads as the square of the blocks.
+// Placing without and with the scan, us: 4,096 blocks 13.9 and 12.3, 8,192 38.9 and 19.1, 32,768 441 and 57; 2,048 blocks take
+// 9.0 without, and a scan is 5 by itself.
+constexpr int32_t kScanBlocks = 2048;
+constexpr int kScanThreads = 1024;
+template <typename T>
+__global__ __launch_bounds__(kScanThreads) void scan_blocks_kernel(LossArgs a, int32_t blocks) {
+    constexpr int kEach = 4;
+    __shared__ uint32_t s_scan[kScanThreads / kWave + 1];
+    __shared__ float s_weight[kScanThreads / kWave];
+    uint32_t before = 0, bad = 0;
+    float top = 0.f;
+    for (int64_t b0 = 0; b0 < blocks; b0 += kScanThreads * kEach) {
+        const int64_t mine = b0 + (int64_t)threadIdx.x * kEach;
+        uint32_t live[kEach], sum = 0, all;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            live[i] = 0;
+            if (mine + i < blocks) {
+                live[i] = a.block_live[mine + i];
+                bad |= a.block_bad[mine + i];
+                top = fmaxf(top, a.block_weight[mine + i]);
+            }
+            sum += live[i];
+        }
+        uint32_t at = before + block_exclusive_scan<uint32_t, kScanThreads>(sum, s_scan, &all);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (mine + i < blocks) a.block_live[mine + i] = at;
+            at += live[i];
+        }
+        before += all;
+        __syncthreads();  // s_scan is used again
+    }
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    if (lane_id() == 0) s_weight[wave_id()] = top;
+    bad = __syncthreads_or(bad != 0);
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < kScanThreads / kWave; ++i) top = fmaxf(top, s_weight[i]);
+    write_header<T>(a, before, bad, top);
+}
+
 // Deals out places: rows with labels from the front, the others behind them.
 template <typename T>
 __global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks) {
@@ -79,7 +133,10 @@ __global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks
     const int64_t row = (int64_t)blockIdx.x * kTile + threadIdx.x;
     bool bad = false;
     const int32_t c = row < a.n ? labels_of_row(a, row, &bad) : 0;
-    if (blocks == 1) {  // nothing was counted
+    const bool scanned = blocks > kScanBlocks;
+    if (scanned) {
+        before = threadIdx.x == 0 ? a.block_live[blockIdx.x] : 0;
+    } else if (blocks == 1) {  // nothing was counted
         all = c > 0;
         bad_any = bad;
         top = c > 0 ? weight_size(a, row) : 0.f;
@@ -108,17 +165,9 @@ __global__ __launch_bounds__(kTile) void place_kernel(LossArgs a, int32_t blocks
     }
     __syncthreads();
     before = s_before[0] + s_before[1];
-    all = s_all[0] + s_all[1];
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        top = fmaxf(s_weight[0], s_weight[1]);
-        a.header->status = s_bad[0] | s_bad[1];
-        a.header->n_live = all;
-        // fp16 holds 2^-24 to 65,504: the largest product of a weight and a count of labels becomes at most 2^15
-        float scale = 1.f;
-        if (std::is_same<T, f16_t>::value && top > 0.f)
-            scale = exp2f(fminf(fmaxf(floorf(log2f(32768.f / (float)a.k) - log2f(top)), -60.f), 60.f));
-        a.header->scale = scale;
-    }
+    all = scanned ? a.header->n_live : s_all[0] + s_all[1];
+    if (!scanned && blockIdx.x == 0 && threadIdx.x == 0)
+        write_header<T>(a, all, s_bad[0] | s_bad[1], fmaxf(s_weight[0], s_weight[1]));
     if (row >= a.n) return;
     // rows with labels in front of this one
     const int64_t at = before + (wave_id() == 1 ? s_wave[0] : 0u) + (uint32_t)__popcll(lives & lanes_below(lane_id()));
@@ -1303,6 +1352,8 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
     const unsigned blocks = (unsigned)p.blocks;
     const Spread spread = make_spread(p.dp, kChunk / (int)sizeof(T));
     if (blocks > 1) hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kTile), 0, stream, a);
+    if (p.blocks > kScanBlocks)
+        hipLaunchKernelGGL(scan_blocks_kernel<T>, dim3(1), dim3(kScanThreads), 0, stream, a, (int32_t)blocks);
     hipLaunchKernelGGL(place_kernel<T>, dim3(blocks), dim3(kTile), 0, stream, a, (int32_t)blocks);
     hipLaunchKernelGGL(gather_kernel<T>, spread_grid(spread, p.n_pad), dim3(kThreads), 0, stream, a, spread, (const T*)c.x,
                        c.x_stride, rows, c.grad ? (T*)c.dx : nullptr, c.dx_stride);
