@@ -1207,9 +1207,9 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
         // the sweeps run one after the other and share the segments' memory
         size_t held = 0, sums = 0;
         for (int mode = kSweepLse; mode <= (grad ? kSweepDw : kSweepLse); ++mode) {
-            const size_t rows = (size_t)sweep_rows(mode, mode == kSweepDw ? V : n, p.dp);
+            const size_t rows = (size_t)sweep_rows(mode, mode == kSweepDw ? V : n, mode == kSweepDw ? n : V, p.dp);
             if (rows > held) held = rows;
-            if (mode != kSweepLse && rows > sums) sums = rows;
+            if (mode > kSweepRest && rows > sums) sums = rows;
         }
         p.o_max = take(held * 4);
         p.o_sum = take(held * 4);

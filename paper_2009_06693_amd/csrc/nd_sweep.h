@@ -141,7 +141,8 @@ struct SweepParts {
     const float* label_sums;
 };
 int sweep_width(int32_t d);                   // numbers in a padded row, 0: rows are too long
-int64_t sweep_rows(int mode, int64_t held, int32_t dp);  // held rows of all segments
+// Held rows of all segments, of as many held and passing rows at most.
+int64_t sweep_rows(int mode, int64_t held, int64_t passing, int32_t dp);
 template <typename T>
 int sweep(int mode, const LossArgs& a, const T* rows, const T* w, int64_t w_stride, const SweepParts& parts, T* dw,
           int64_t dw_stride, hipStream_t stream);

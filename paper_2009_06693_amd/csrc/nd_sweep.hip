@@ -671,9 +671,12 @@ int launch_sweep(const LossArgs& a, const SweepArgs& s, hipStream_t stream) {
 }  // namespace
 
 int sweep_width(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : d <= 256 ? 256 : 0; }
-int64_t sweep_rows(int mode, int64_t held, int32_t dp) {
+int64_t sweep_rows(int mode, int64_t held, int64_t passing, int32_t dp) {
+    // Fewer rows are dealt out to as many workgroups or fewer.  Segments' numbers: by workgroup and tile (both go up by one at a
+    // time), or two of a workgroup.
     const SweepShape shape = sweep_shape(mode, dp);
-    return (mode == kSweepDw ? 2 * shape.groups() : shape.groups() + (held + shape.held() - 1) / shape.held()) * shape.held();
+    const SweepDeal deal(held, passing, shape);
+    return (mode == kSweepDw ? 2 * deal.groups : deal.groups + deal.tiles) * shape.held();
 }
 
 template <typename T>
