@@ -439,9 +439,10 @@ typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
  *   workspace_dev    nd_softmax_loss_workspace_bytes bytes, 256-byte aligned, owned by the caller (grad: for
  *                    nd_softmax_loss_grad); calls that overlap in time need one each
  *
- * Up to 256 16-bit numbers a row no score leaves the registers.  Of longer rows, and in fp32, scores and what is made of
- * them lie in the workspace: at most 512 MB of probabilities at a time, or up to 4 GB of scores where rows are so long that
- * they are cheaper to keep than to make twice.  Before they are multiplied by rows, probabilities are rounded to the type of
+ * Up to 256 16-bit numbers a row no score leaves the registers.  Of longer rows, and in fp32, the gradient's workspace holds
+ * probabilities of a piece of the vertices at a time: 512 MB of them at most, or 256 vertices', 512 n bytes (fp32: 1,024 n),
+ * where that is more.  Where rows are so long (512 16-bit numbers, 128 in fp32) that scores are cheaper to keep than to make
+ * twice, and all of them are 4 GB or less, it holds those as well (fp32: instead).  Before they are multiplied by rows, probabilities are rounded to the type of
  * the rows (fp32: not at all), half a step relative to each.  A row's own labels are not: c_n p - #, small where a row is
  * fitted, is made and multiplied in 32 bits.  fp16: row_weight p is held in steps no finer than 2^-39 k of the largest finite
  * row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status waits for the

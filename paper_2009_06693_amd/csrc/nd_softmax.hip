@@ -21,7 +21,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = 128;         // rows of a product's tile
 constexpr int kChunk = 16;         // bytes that a lane moves at once
-constexpr size_t kPieceBytes = (size_t)512 << 20;  // probabilities that lie in the workspace at a time, where scores are not kept
+// Probabilities that lie in the workspace at a time: so many, or those of one tile of vertices where rows are more than a million
+// (fp32: half as many).  fp32 scores that are kept have theirs in their place.
+constexpr size_t kPieceBytes = (size_t)512 << 20;
 constexpr int64_t kKeptBytes = (int64_t)4 << 30;    // scores that are kept at most
 
 typedef float Acc __attribute__((ext_vector_type(16)));
@@ -882,13 +884,13 @@ void probs_kernel(LossArgs a, Operand<T> w, Operand<T> x, int64_t v_first,
         }
 }
 
-// The same from scores that were kept; fp32: in their place.  A lane has four places.
+// The same from scores that were kept, of the piece of vertices from v_first on; fp32: in their place.  A lane has four places.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float* scores, T* probs) {
+__global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float* scores, int64_t v_first, T* probs) {
     __shared__ __align__(16) uint8_t counts[Kind<T>::kWide ? kTile * kCountPitch : 16];
     constexpr int kLanes = kTile / 4, kRows = kThreads / kLanes, kAtOnce = 8;
     const int64_t id = tile_id(), blocks = a.n_pad / kTile;
-    const int64_t n0 = id % blocks * kTile, v0 = id / blocks * kTileM;
+    const int64_t n0 = id % blocks * kTile, m0 = id / blocks * kTileM, v0 = v_first + m0;
     if (n0 >= (int64_t)a.header->n_live) return;
     if constexpr (Kind<T>::kWide) count_labels(a, v0, n0, counts);
     const float scale = a.header->scale;
@@ -918,7 +920,7 @@ __global__ __launch_bounds__(kThreads) void kept_kernel(LossArgs a, const float*
                         p.v[e] = weight_of<T>(s[i].v[e], lse[e], c[e], g[e]);
                 }
             }
-            store_piece<T, 4>(probs + (v0 + row) * a.n_pad + n0 + col, p);
+            store_piece<T, 4>(probs + (m0 + row) * a.n_pad + n0 + col, p);
         }
     }
 }
@@ -1152,7 +1154,7 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     // 4,096 x 57,000 x 64 713 and 709.
     p.kept = grad && !p.sweep && v_tiles <= 32768 && p.n_pad * v_tiles * kTileM * 4 <= kKeptBytes &&
              p.dp >= (dtype == ND_F32 ? 128 : 512);
-    if (p.kept) piece_tiles = v_tiles;
+    if (p.kept && dtype == ND_F32) piece_tiles = v_tiles;  // probabilities take the scores' place
     p.piece = piece_tiles * kTileM;
     // The summed dimension is shared out where there are fewer tiles than two per compute unit; one more share than that
     // would take as long as twice as many.  More than 16 shares cost more to join than the second workgroup of a compute
@@ -1223,7 +1225,7 @@ LossPlan plan_loss(int64_t n, int64_t V, int32_t d, int32_t k, int dtype, bool g
     if (grad) {
         if (dtype != ND_F32) take_labels();
         p.o_probs = take((size_t)p.piece * (size_t)p.n_pad * (size_t)b);
-        p.o_scores = p.kept && b < 4 ? take((size_t)p.piece * (size_t)p.n_pad * 4) : p.o_probs;
+        p.o_scores = p.kept && b < 4 ? take((size_t)(v_tiles * kTileM) * (size_t)p.n_pad * 4) : p.o_probs;
         p.o_parts = take((size_t)p.shares * (size_t)p.n_pad * (size_t)p.dp * 4);
         p.o_dw_parts = p.dw_shares > 1 ? take((size_t)p.dw_shares * (size_t)p.piece * (size_t)p.dp * 4) : 0;
     }
@@ -1416,7 +1418,7 @@ int run_loss(const LossCall& c, const LossPlan& p, char* ws, hipStream_t stream)
             const Operand<T> op{probs, p.n_pad, tiles * kTileM, (int32_t)p.n_pad};
             const dim3 all((unsigned)(p.n_pad / kTile * tiles));
             if (c.n > 0 && p.kept)
-                hipLaunchKernelGGL(kept_kernel<T>, all, dim3(kThreads), 0, stream, a, (const float*)(ws + p.o_scores), probs);
+                hipLaunchKernelGGL(kept_kernel<T>, all, dim3(kThreads), 0, stream, a, (const float*)(ws + p.o_scores), v, probs);
             else if (c.n > 0)
                 hipLaunchKernelGGL(probs_kernel<T>, all, dim3(kThreads), 0, stream, a, ow, ox, v, probs);
             if (c.dw)

@@ -38,3 +38,8 @@ def _check(n, V, d, k, kind):
                                  (2000, 90)])
 def test_rows_of_sweeps(n, V, d, kind):
     _check(n, V, d, 2, kind)
+
+
+@pytest.mark.parametrize("kind,n,V,d", [("bf16", 4600, 70000, 520), ("f16", 2100, 140000, 600), ("f32", 1200, 3000, 200)])
+def test_kept_scores_whose_probabilities_come_in_pieces(n, V, d, kind):
+    _check(n, V, d, 2, kind)
