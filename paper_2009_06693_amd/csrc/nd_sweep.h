@@ -25,7 +25,7 @@ struct SweepShape {
 };
 constexpr SweepShape sweep_shape(int mode, int d) {
     // Registers leave room for two workgroups where few sums are kept: 14,250 x 57,000 x 128 forward 230 us, 248 with one;
-    // over rows of 64 numbers 159 and 187, with dx (8,192 rows) 138 and 152.
+    // over rows of 64 numbers 159 and 187, with dx (8,192 rows of ten labels) 146 and 163.
     if (mode <= kSweepRest) return d > 128 ? SweepShape{8, 64, 1} : SweepShape{8, 64, 2};
     if (mode == kSweepDx && d <= 64) return SweepShape{8, 64, 2};
     // two of these blocks of 32 rows are a unit of the others

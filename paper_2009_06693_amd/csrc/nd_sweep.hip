@@ -18,10 +18,10 @@
 // what it rounded to and the difference from the count, both in 32 bits.
 //
 // What bounds it: matrix instructions and vector instructions share a SIMD's issue (an instruction of 32 cycles keeps it for
-// 16), and under both the clock falls below 2 GHz.  8,192 x 57,000 x 128 bf16: with dx 260 us (225 where no label is left out; here
-// 74,000 are, two fifths of them in an eighth of the vertices, and the workgroups that sweep those end last), dw 231, 920 and
-// 1,035 TFLOP/s of products beside an exponential for every score; forward, 14,250 x 57,000 x 128 fp16, 229 us, 908; 8,192 x
-// 233,000 x 256 1,670 and 1,880 us.
+// 16), and under both the clock falls below 2 GHz.  8,192 x 57,000 x 128 bf16: with dx 250 us and dw 229, 956 and 1,044 TFLOP/s of
+// products beside an exponential for every score; forward, 14,250 x 57,000 x 128 fp16, 229 us, 908; 8,192 x 233,000 x 256 1,640 and
+// 1,760 us.  dx is 220 us where rows have one label: of ten, two fifths fall into an eighth of the vertices here, and the
+// workgroups that sweep those end last.
 namespace nd {
 namespace {
 
@@ -290,7 +290,8 @@ void sweep_kernel(LossArgs a, SweepArgs s) {
                 if (half * 4 >= rows_left - (b * 32 + 8 * (r / 4) + r % 4)) now[r] = -INFINITY;
         };
         // ---- Labels among the block's rows weigh nothing here: what they are in the gradient is put together in 32 bits where
-        // the segments are joined.  Few blocks hold one: the others cost a comparison.
+        // the segments are joined.  Few blocks hold one: the others cost a comparison.  The label after the next is on its way
+        // (260 us; 277 where each was fetched when the one before it was found).
         auto leave_out = [&](Acc& now, int32_t u, int b) {
             const uint32_t first = (uint32_t)u * UNIT + (uint32_t)b * 32u;
             if (!__ballot(label - first < 32u)) return;
