@@ -442,11 +442,11 @@ typedef enum nd_dtype { ND_F32 = 0, ND_BF16 = 1, ND_F16 = 2 } nd_dtype;
  * Up to 256 16-bit numbers a row no score leaves the registers.  Of longer rows, and in fp32, the gradient's workspace holds
  * probabilities of a piece of the vertices at a time: 512 MB of them at most, or 256 vertices', 512 n bytes (fp32: 1,024 n),
  * where that is more.  Where rows are so long (512 16-bit numbers, 128 in fp32) that scores are cheaper to keep than to make
- * twice, and all of them are 4 GB or less, it holds those as well (fp32: instead).  Before they are multiplied by rows, probabilities are rounded to the type of
- * the rows (fp32: not at all), half a step relative to each.  A row's own labels are not: c_n p - #, small where a row is
- * fitted, is made and multiplied in 32 bits.  fp16: row_weight p is held in steps no finer than 2^-39 k of the largest finite
- * row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status waits for the
- * stream and returns ND_ERR_BAD_ROOT then.  Infinities and NaN in a row of x stay in that row's loss, lse and dx.
+ * twice, and all of them are 4 GB or less, it holds those as well (fp32: instead).  Before they are multiplied by rows,
+ * probabilities are rounded to the type of the rows (fp32: not at all), half a step relative to each.  A row's own labels are
+ * not: c_n p - #, small where a row is fitted, is made and multiplied in 32 bits.  fp16: row_weight p is held in steps no finer
+ * than 2^-39 k of the largest finite row weight.  A label of V or more counts as NULL and is recorded: nd_softmax_loss_status
+ * waits for the stream and returns ND_ERR_BAD_ROOT then.  Infinities and NaN in a row of x stay in that row's loss, lse and dx.
  * Limits: n < 2^30, V < 2^31, d <= ND_MAX_ROW, k <= ND_MAX_LABELS, n * k < 2^31.  Errors: ND_ERR_NULL_POINTER,
  * ND_ERR_BAD_ARGUMENT, ND_ERR_TOO_LARGE, ND_ERR_WORKSPACE, ND_ERR_HIP.
  */
